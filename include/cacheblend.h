@@ -264,6 +264,80 @@ int cb_fuse_prefill_batched(cb_ctx *ctx, const cb_layer_weights *layers, int32_t
 int cb_first_token(cb_ctx *ctx, const float *final_hidden, int32_t n_suffix, const void *final_norm,
                    const void *lm_head, int32_t vocab, float *logits, int32_t *token, void *stream);
 
+/* ---- Several continuations of one fused context ------------------------------------------------------------------
+ * After the prefill a request goes on one token at a time, often along several continuations at once: the beams of a beam
+ * search, several sampled answers, several questions about the same documents.  They share the fused context, which is
+ * stored once, and each has a TAIL of its own: rows of T [n_kv_heads, head_dim] in slabs of tail_stride rows, continuation b
+ * of group g in slab g * n_seqs + b of the tail arrays (one K and one V array per layer).  A group is the
+ * continuations of one request.  A decoding step of a layer projects Q, K and V of the new tokens, then calls
+ * cb_qkv_norm_rope and cb_shared_prefix_attention; after the last layer come the vocabulary projection, cb_beam_select and,
+ * for all layers at once, cb_beam_reorder.  Lengths that change from step to step are device arrays, so that a step
+ * can be captured into a graph once.  Needs a stream of the device the ctx was created on (else CB_EINVAL), as cb_first_token. */
+
+/* Queries and keys of new tokens: per-head RMSNorm (eps = desc.rms_eps; left out where its gain is NULL), rotation by the token's
+ * position in the ctx's rotary order (Appendix A), rounded once after both; the rotated keys and the values go into the cache.
+ *   q, k, v   : T, token r's heads at q + r * q_stride (k, v likewise), strides in elements, multiples of 16 bytes -- the three
+ *               may be columns of one projection's output
+ *   q_norm, k_norm : NULL, or T [head_dim], the gain that all query / key heads share
+ *   row_pos   : int32 [n_rows] position of every token.  One outside 0 .. max_tokens - 1 marks a padding row: nothing is
+ *               written for it
+ *   cache_row : int32 [n_rows] row of the cache arrays that receives the token's K and V, outside 0 .. n_cache_rows - 1: not
+ *               stored.  Two tokens with the same row leave a mixture of theirs in it
+ *   q_out     : T [n_rows, n_q_heads, head_dim]; may be q itself if q_stride = n_q_heads * head_dim
+ *   k_cache, v_cache : T [n_cache_rows, n_kv_heads, head_dim]; other rows are left as they were */
+int cb_qkv_norm_rope(cb_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                     const void *q_norm, const void *k_norm, const int32_t *row_pos, const int32_t *cache_row, int32_t n_rows,
+                     void *q_out, void *k_cache, void *v_cache, int64_t n_cache_rows, void *stream);
+
+/* Attention of n_groups x n_seqs continuations, n_q query rows each (1 for a decoding step; more for questions or drafted
+ * tokens, ragged ones padded): a query sees its group's context and the first row_tail rows of its continuation's tail.  The
+ * context is read once for all of a group's continuations.
+ *   q, o       : T [n_groups * n_seqs * n_q, n_q_heads, head_dim], continuation after continuation; o may be q itself
+ *   k_prefix, v_prefix : T, group g's context in rows g * prefix_stride .. + prefix_lens[g] (the fused caches that cb_fuse_prefill
+ *                leaves, n_groups = 1; those of cb_fuse_prefill_batched, prefix_stride = cache_stride)
+ *   prefix_lens : HOST int32 [n_groups], 0 <= prefix_lens[g] <= prefix_stride
+ *   k_tail, v_tail : T [n_groups * n_seqs * tail_stride, n_kv_heads, head_dim]
+ *   row_tail   : int32 [n_groups * n_seqs * n_q]: tail rows the query sees, at most tail_stride (more count as that), the query's
+ *                own token among them; negative: a padding row
+ * A padding row, and one that sees no key at all, gets zeros.  Hidden rows have no influence, whatever they hold (infinities and
+ * NaN included).  Softmax statistics and sums are float; results do not depend on which continuations share the call but for
+ * the order of additions.  prefix_stride = 0 / tail_stride = 0: no contexts / tails, their pointers are ignored.
+ * The workspace bytes for max_prefix hold for every shorter context; 0: arguments out of range. */
+size_t cb_shared_prefix_workspace_bytes(const cb_ctx *ctx, int32_t n_groups, int32_t n_seqs, int32_t n_q, int32_t max_prefix,
+                                        int32_t tail_stride);
+int cb_shared_prefix_attention(cb_ctx *ctx, const void *q, int32_t n_groups, int32_t n_seqs, int32_t n_q, const void *k_prefix,
+                               const void *v_prefix, const int32_t *prefix_lens /*HOST*/, int32_t prefix_stride, const void *k_tail,
+                               const void *v_tail, int32_t tail_stride, const int32_t *row_tail, void *o, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/* The best continuations of every group: the n_keep largest of
+ *     scores[beam] + logits[beam][token] - log sum_t exp(logits[beam][t])
+ * over the group's beams and the vocabulary, largest first, equal ones by lower beam, then lower token; within a beam the order is
+ * that of the logits.  Scores are compared in double.
+ *   logits    : logits_dtype (cb_dtype, need not be T), row r = group * n_beams + beam at logits + r * row_stride (elements); any
+ *               alignment of its type.  NaN counts as -infinity; infinite logits share their beam's probability
+ *   scores    : float [n_groups * n_beams], the beams' sums so far; -infinity or NaN: a beam that is not there
+ *   finished  : NULL, or int32 [n_groups * n_beams]: a beam with a value other than 0 has ended; its logits are not looked at, it goes
+ *               on as one continuation with its score unchanged and the token end_token (0 <= end_token < vocab)
+ *   scores_out, beam_out, token_out : float, int32, int32 [n_groups * n_keep]; beam_out counts within the group.  Where a group has
+ *               fewer continuations above -infinity, the rest are (-infinity, -1, -1).  None may overlap an input
+ * 1 <= n_keep <= 64 and n_beams <= 64 (else CB_EUNSUPPORTED, as n_groups * n_beams > 65535). */
+size_t cb_beam_select_workspace_bytes(const cb_ctx *ctx, int32_t n_groups, int32_t n_beams, int32_t vocab, int32_t n_keep);
+int cb_beam_select(cb_ctx *ctx, const void *logits, int32_t logits_dtype, int64_t row_stride, int32_t n_groups, int32_t n_beams,
+                   int32_t vocab, const float *scores, const int32_t *finished, int32_t end_token, int32_t n_keep, float *scores_out,
+                   int32_t *beam_out, int32_t *token_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The beams' tails follow the survivors, in place and for all beams at once: rows 0 .. seq_len[parent] - 1 of the parent's slab become those
+ * of the beam's, on layers layer_begin .. layer_end - 1.  Rows behind stay as they were; a beam that is its own parent, or whose parent lies
+ * outside 0 .. n_beams - 1 (beam_out's -1), keeps its slab.  Lengths are the parents' and in the old order: reordering them is the caller's.
+ *   k_tail_layers, v_tail_layers : HOST arrays [n_layers] of device pointers to T [n_groups * n_beams * tail_stride, n_kv_heads,
+ *               head_dim], all different
+ *   parent    : int32 [n_groups * n_beams], counted within the group
+ *   seq_len   : int32 [n_groups * n_beams] (0 .. tail_stride), or NULL: whole slabs
+ * n_beams <= 64, n_groups <= 65535 (else CB_EUNSUPPORTED). */
+int cb_beam_reorder(cb_ctx *ctx, void *const *k_tail_layers, void *const *v_tail_layers, int32_t layer_begin, int32_t layer_end,
+                    int32_t n_groups, int32_t n_beams, int32_t tail_stride, const int32_t *parent, const int32_t *seq_len, void *stream);
+
 /* Loading controller (Sec. 5.1).  Plain host arithmetic, no ctx, no device work.
  * cb_recompute_delay: T_recompute = ratio x profiled full-prefill delay (first footnote).
  * cb_load_delay     : T_load = per-token KV bytes x tokens / device throughput, in seconds

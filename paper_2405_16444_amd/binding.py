@@ -80,6 +80,15 @@ def _load():
                                             C.POINTER(i32), C.POINTER(vp), C.POINTER(vp), i32, C.POINTER(i32),
                                             vp, C.POINTER(vp), C.POINTER(vp), vp, sz, vp]
     lib.cb_first_token.argtypes = [vp, vp, i32, vp, vp, i32, vp, vp, vp]
+    i64 = C.c_int64
+    lib.cb_qkv_norm_rope.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i32, vp, vp, vp, i64, vp]
+    lib.cb_shared_prefix_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, i32]
+    lib.cb_shared_prefix_workspace_bytes.restype = sz
+    lib.cb_shared_prefix_attention.argtypes = [vp, vp, i32, i32, i32, vp, vp, C.POINTER(i32), i32, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.cb_beam_select_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
+    lib.cb_beam_select_workspace_bytes.restype = sz
+    lib.cb_beam_select.argtypes = [vp, vp, i32, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.cb_beam_reorder.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), i32, i32, i32, i32, i32, vp, vp, vp]
     dbl = C.c_double
     lib.cb_recompute_delay.argtypes = [dbl, dbl]
     lib.cb_recompute_delay.restype = dbl
@@ -99,8 +108,9 @@ _lib = _load()
 EXPORTS = ("cb_create", "cb_destroy", "cb_strerror", "cb_layer_workspace_bytes",
            "cb_prefill_workspace_bytes", "cb_default_schedule", "cb_realign_rope", "cb_fuse_layer",
            "cb_static_scratch_bytes", "cb_fuse_layer_static", "cb_fuse_prefill", "cb_fuse_prefill_pipelined", "cb_batched_workspace_bytes",
-           "cb_fuse_prefill_batched", "cb_first_token", "cb_recompute_delay", "cb_load_delay",
-           "cb_pick_recompute_ratio", "cb_pick_storage_device", "cb_profile_enable", "cb_profile_read")
+           "cb_fuse_prefill_batched", "cb_first_token", "cb_qkv_norm_rope", "cb_shared_prefix_workspace_bytes",
+           "cb_shared_prefix_attention", "cb_beam_select_workspace_bytes", "cb_beam_select", "cb_beam_reorder",
+           "cb_recompute_delay", "cb_load_delay", "cb_pick_recompute_ratio", "cb_pick_storage_device", "cb_profile_enable", "cb_profile_read")
 
 
 def _check(status: int, where: str):
@@ -427,6 +437,141 @@ def cb_first_token(ctx: Context, final_hidden: torch.Tensor, final_norm: torch.T
     _check(_lib.cb_first_token(ctx._h, _ptr(final_hidden), n_suffix, _ptr(final_norm), _ptr(lm_head), vocab,
                                _ptr(logits), _ptr(token), _stream(stream)), "cb_first_token")
     return logits, token
+
+
+def _caches(ctx: Context, k: torch.Tensor, v: torch.Tensor):
+    """Checks a K and a V array [rows, Hkv, dh] of the context's type."""
+    m = ctx.model
+    assert k.dtype == ctx.dtype and v.dtype == ctx.dtype and k.is_contiguous() and v.is_contiguous()
+    assert k.shape == v.shape and k.shape[1:] == (m.n_kv_heads, m.head_dim) and k.device == ctx.device and v.device == ctx.device
+
+
+def cb_qkv_norm_rope(ctx: Context, qkv, row_pos: torch.Tensor, cache_row: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                     q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None,
+                     q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Normalised, rotated queries [n_rows, Hq, dh] (returned); keys and values go into rows cache_row of the caches.
+    qkv: one projection output [n_rows, (Hq + 2 Hkv) dh], or the three as (q, k, v); rows may be strided."""
+    m, dev = ctx.model, ctx.device
+    dh, nq, nk = m.head_dim, m.n_q_heads * m.head_dim, m.n_kv_heads * m.head_dim
+    if isinstance(qkv, torch.Tensor):
+        n_rows, width = qkv.shape
+        assert qkv.dtype == ctx.dtype and qkv.device == dev and width == nq + 2 * nk and (qkv.stride(1) == 1 or n_rows == 0)
+        qs = ks = vs = qkv.stride(0) if n_rows > 1 else width
+        es, q = qkv.element_size(), qkv.data_ptr()
+        k, v = q + nq * es, q + (nq + nk) * es
+    else:
+        n_rows = qkv[0].shape[0]
+        for t, w in zip(qkv, (nq, nk, nk)):
+            assert t.dtype == ctx.dtype and t.device == dev and t.shape == (n_rows, w) and (t.stride(1) == 1 or n_rows == 0)
+        q, k, v = (t.data_ptr() for t in qkv)
+        qs, ks, vs = (t.stride(0) if n_rows > 1 else w for t, w in zip(qkv, (nq, nk, nk)))
+    for t in (row_pos, cache_row):
+        assert t.dtype == torch.int32 and t.shape == (n_rows,) and t.is_contiguous() and t.device == dev
+    for t in (q_norm, k_norm):
+        assert t is None or (t.dtype == ctx.dtype and t.shape == (dh,) and t.is_contiguous() and t.device == dev)
+    _caches(ctx, k_cache, v_cache)
+    if q_out is None:
+        q_out = torch.empty((n_rows, m.n_q_heads, dh), dtype=ctx.dtype, device=dev)
+    assert q_out.dtype == ctx.dtype and q_out.device == dev and q_out.is_contiguous() and q_out.shape == (n_rows, m.n_q_heads, dh)
+    _check(_lib.cb_qkv_norm_rope(ctx._h, q, qs, k, ks, v, vs, _ptr(q_norm), _ptr(k_norm), row_pos.data_ptr(), cache_row.data_ptr(),
+                                 n_rows, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_cache.shape[0], _stream(stream)),
+           "cb_qkv_norm_rope")
+    return q_out
+
+
+def cb_shared_prefix_workspace_bytes(ctx: Context, n_groups: int, n_seqs: int, n_q: int, max_prefix: int, tail_stride: int) -> int:
+    return int(_lib.cb_shared_prefix_workspace_bytes(ctx._h, n_groups, n_seqs, n_q, max_prefix, tail_stride))
+
+
+def cb_shared_prefix_attention(ctx: Context, q: torch.Tensor, n_groups: int, n_seqs: int, n_q: int, k_prefix: torch.Tensor,
+                               v_prefix: torch.Tensor, prefix_lens: Sequence[int], k_tail: torch.Tensor, v_tail: torch.Tensor,
+                               row_tail: torch.Tensor, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                               stream=None) -> torch.Tensor:
+    """Attention of n_groups x n_seqs continuations over their group's context and their own tails.  q [rows, Hq, dh]; k_prefix / v_prefix
+    [n_groups * prefix_stride, Hkv, dh]; k_tail / v_tail [n_groups * n_seqs * tail_stride, Hkv, dh]; row_tail int32 [rows]."""
+    m, dev = ctx.model, ctx.device
+    seqs = n_groups * n_seqs
+    rows = seqs * n_q
+    assert n_groups >= 1 and n_seqs >= 1 and n_q >= 1 and len(prefix_lens) == n_groups
+    assert q.dtype == ctx.dtype and q.device == dev and q.is_contiguous() and q.shape == (rows, m.n_q_heads, m.head_dim)
+    assert row_tail.dtype == torch.int32 and row_tail.shape == (rows,) and row_tail.is_contiguous() and row_tail.device == dev
+    _caches(ctx, k_prefix, v_prefix)
+    _caches(ctx, k_tail, v_tail)
+    assert k_prefix.shape[0] % n_groups == 0 and k_tail.shape[0] % seqs == 0
+    prefix_stride, tail_stride = k_prefix.shape[0] // n_groups, k_tail.shape[0] // seqs
+    if out is None:
+        out = torch.empty_like(q)
+    assert out.dtype == ctx.dtype and out.device == dev and out.is_contiguous() and out.shape == q.shape
+    if workspace is None:
+        workspace = torch.empty(cb_shared_prefix_workspace_bytes(ctx, n_groups, n_seqs, n_q, max(prefix_lens), tail_stride),
+                                dtype=torch.uint8, device=dev)
+    _check(_lib.cb_shared_prefix_attention(ctx._h, q.data_ptr(), n_groups, n_seqs, n_q, k_prefix.data_ptr(), v_prefix.data_ptr(),
+                                           (C.c_int32 * n_groups)(*prefix_lens), prefix_stride, k_tail.data_ptr(), v_tail.data_ptr(),
+                                           tail_stride, row_tail.data_ptr(), out.data_ptr(), workspace.data_ptr(),
+                                           workspace.numel(), _stream(stream)), "cb_shared_prefix_attention")
+    return out
+
+
+def cb_beam_select_workspace_bytes(ctx: Context, n_groups: int, n_beams: int, vocab: int, n_keep: int) -> int:
+    return int(_lib.cb_beam_select_workspace_bytes(ctx._h, n_groups, n_beams, vocab, n_keep))
+
+
+def cb_beam_select(ctx: Context, logits: torch.Tensor, scores: torch.Tensor, n_groups: int, n_keep: int,
+                   finished: Optional[torch.Tensor] = None, end_token: int = 0, workspace: Optional[torch.Tensor] = None, stream=None,
+                   out=None):
+    """(scores float, beam int32, token int32), each [n_groups, n_keep], best first.  logits [n_groups * n_beams, vocab] float or bfloat16,
+    rows may be strided; scores float [n_groups * n_beams]; finished None or int32 of the same size.  out: the three results' tensors."""
+    dev = ctx.device
+    rows, vocab = logits.shape
+    assert n_groups >= 1 and rows >= n_groups and rows % n_groups == 0 and logits.device == dev
+    assert logits.dtype in (torch.float32, torch.bfloat16) and (logits.stride(1) == 1 or vocab == 1)
+    assert scores.dtype == torch.float32 and scores.numel() == rows and scores.is_contiguous() and scores.device == dev
+    if finished is not None:
+        assert finished.dtype == torch.int32 and finished.numel() == rows and finished.is_contiguous() and finished.device == dev
+    if out is None:
+        out = (torch.empty((n_groups, n_keep), dtype=torch.float32, device=dev),
+               torch.empty((n_groups, n_keep), dtype=torch.int32, device=dev),
+               torch.empty((n_groups, n_keep), dtype=torch.int32, device=dev))
+    for t, dt in zip(out, (torch.float32, torch.int32, torch.int32)):
+        assert t.dtype == dt and t.numel() == n_groups * n_keep and t.is_contiguous() and t.device == dev
+    n_beams = rows // n_groups
+    if workspace is None:
+        workspace = torch.empty(max(256, cb_beam_select_workspace_bytes(ctx, n_groups, n_beams, vocab, n_keep)), dtype=torch.uint8,
+                                device=dev)
+    _check(_lib.cb_beam_select(ctx._h, logits.data_ptr(), CB_F32 if logits.dtype == torch.float32 else CB_BF16,
+                               logits.stride(0) if rows > 1 else vocab, n_groups, n_beams, vocab, scores.data_ptr(), _ptr(finished),
+                               end_token, n_keep, out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), workspace.data_ptr(),
+                               workspace.numel(), _stream(stream)), "cb_beam_select")
+    return out
+
+
+def _layer_ptrs(ctx: Context, layers):
+    """Pointers of per-layer arrays [rows, Hkv, dh]: a sequence of tensors, or one tensor with the layers in front; and their rows."""
+    m = ctx.model
+    if isinstance(layers, torch.Tensor):
+        assert layers.dtype == ctx.dtype and layers.is_contiguous() and layers.device == ctx.device
+        assert layers.dim() == 4 and layers.shape[2:] == (m.n_kv_heads, m.head_dim)
+        n, base, step = layers.shape[0], layers.data_ptr(), layers.stride(0) * layers.element_size()
+        return (C.c_void_p * n)(*[base + i * step for i in range(n)]), n, layers.shape[1]
+    rows = layers[0].shape[0]
+    for t in layers:
+        assert t.dtype == ctx.dtype and t.is_contiguous() and t.device == ctx.device
+        assert t.shape == (rows, m.n_kv_heads, m.head_dim)
+    return _ptr_array(layers), len(layers), rows
+
+
+def cb_beam_reorder(ctx: Context, k_tail_layers, v_tail_layers, n_groups: int, parent: torch.Tensor,
+                    seq_len: Optional[torch.Tensor] = None, stream=None):
+    """The beams' tails follow their parents, in place.  k_tail_layers / v_tail_layers: per layer [n_groups * n_beams * tail_stride, Hkv, dh],
+    as a sequence of tensors or one tensor [layers, ...]; at most the model's layers.  parent, seq_len: int32 [n_groups * n_beams]."""
+    k, nk, rows = _layer_ptrs(ctx, k_tail_layers)
+    v, nv, rows_v = _layer_ptrs(ctx, v_tail_layers)
+    beams = parent.numel()
+    assert nk == nv and rows == rows_v and n_groups >= 1 and beams >= n_groups and beams % n_groups == 0 and rows % beams == 0
+    for t in (parent, seq_len):
+        assert t is None or (t.dtype == torch.int32 and t.numel() == beams and t.is_contiguous() and t.device == ctx.device)
+    _check(_lib.cb_beam_reorder(ctx._h, k, v, 0, nk, n_groups, beams // n_groups, rows // beams, parent.data_ptr(), _ptr(seq_len),
+                                _stream(stream)), "cb_beam_reorder")
 
 
 def cb_recompute_delay(ratio: float, prefill_delay: float) -> float:

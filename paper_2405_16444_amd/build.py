@@ -10,7 +10,8 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libcacheblend.so")
-SOURCES = ["elementwise.hip", "select.hip", "gemm.hip", "attention.hip", "head.hip", "api.hip"]
+SOURCES = ["elementwise.hip", "select.hip", "gemm.hip", "attention.hip", "head.hip", "beams.hip",
+           "shared_attention.hip", "api.hip"]
 # packed-fp32 VALU forms are disabled on purpose (some of them have given wrong results)
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

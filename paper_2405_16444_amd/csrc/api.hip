@@ -277,6 +277,15 @@ int stage_weights(cb_ctx *c, hipStream_t s, const LayerWs &ws, int n, const void
 // k context rows are kept, its caches hold T rows.
 struct Seg { int n, S, k, T; };
 
+// A stream of the ctx's device (the default stream and the runtime's special handles, small integers, stand for streams of the
+// current device and are no objects to ask).
+int check_stream(const cb_ctx *c, hipStream_t s) {
+  int device = -1;
+  const bool object = reinterpret_cast<uintptr_t>(s) > 16;
+  if ((object ? hipStreamGetDevice(s, &device) : hipGetDevice(&device)) != hipSuccess) return CB_EHIP;
+  return device == c->device ? CB_OK : CB_EINVAL;
+}
+
 // runs a projection: the main launch and, when its sums were parked, the finish launch
 int run_gemm(cb_ctx *c, hipStream_t s, const GemmArgs &g, int finish_class, double flops, double bytes,
              double finish_bytes) {
@@ -1025,16 +1034,166 @@ int cb_first_token(cb_ctx *c, const float *final_hidden, int32_t n_suffix, const
   const int d = c->m.d_model;
   if (d % 8 != 0 || d > 16384) return CB_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
-  // the launch updates c->pick, which only the ctx's device is sure to reach (the default stream and the runtime's special
-  // handles, small integers, stand for streams of the current device and are no objects to ask)
-  int device = -1;
-  const bool object = reinterpret_cast<uintptr_t>(s) > 16;
-  if ((object ? hipStreamGetDevice(s, &device) : hipGetDevice(&device)) != hipSuccess) return CB_EHIP;
-  if (device != c->device) return CB_EINVAL;
+  CB_TRY(check_stream(c, s));           // the launch updates c->pick, which only the ctx's device is sure to reach
   const size_t es = esize(c);
   ProfScope ps(c, s, CB_PROF_HEAD, 2.0 * vocab * d, (double)vocab * d * es + (double)vocab * 4);
   CB_HIP(launch_lm_head(c->m.dtype, final_hidden + (size_t)(n_suffix - 1) * d, final_norm, lm_head, d, vocab,
                         c->m.rms_eps, logits, token, c->pick, s));
+  return CB_OK;
+}
+
+int cb_qkv_norm_rope(cb_ctx *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                     const void *q_norm, const void *k_norm, const int32_t *row_pos, const int32_t *cache_row, int32_t n_rows,
+                     void *q_out, void *k_cache, void *v_cache, int64_t n_cache_rows, void *stream) {
+  if (!c) return CB_ENULL;
+  if (n_rows < 0 || n_cache_rows < 0) return CB_EINVAL;
+  if (n_rows == 0) return CB_OK;
+  if (!q || !k || !v || !row_pos || !cache_row || !q_out || !k_cache || !v_cache) return CB_ENULL;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_norm, 16) || !aligned(k_norm, 16) ||
+      !aligned(row_pos, 4) || !aligned(cache_row, 4) || !aligned(q_out, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16))
+    return CB_EINVAL;
+  const cb_model_desc &m = c->m;
+  const int64_t es = (int64_t)esize(c), q_dim = (int64_t)m.n_q_heads * m.head_dim, kv_dim = (int64_t)m.n_kv_heads * m.head_dim;
+  if (q_stride < q_dim || k_stride < kv_dim || v_stride < kv_dim || q_stride * es % 16 || k_stride * es % 16 || v_stride * es % 16)
+    return CB_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  CB_TRY(check_stream(c, s));
+  QkvRows a = {q, k, v, q_stride, k_stride, v_stride, q_norm, k_norm, row_pos, cache_row, q_out, k_cache, v_cache, n_cache_rows,
+               c->rope_tab, m.dtype, n_rows, m.n_q_heads, m.n_kv_heads, m.head_dim, m.rope_layout == CB_ROPE_HALF, c->max_tokens,
+               m.rms_eps};
+  ProfScope ps(c, s, CB_PROF_NORM, 0, 2.0 * n_rows * (double)(q_dim + 2 * kv_dim) * es);
+  CB_HIP(launch_qkv_norm_rope(a, s));
+  return CB_OK;
+}
+
+namespace {
+// Fills in the shapes of an attention call and plans it; false: more rows or slots than the launches number.
+bool plan_shared(const cb_ctx *c, int n_groups, int n_seqs, int n_q, int max_ctx, int tail_stride, SharedAttn *a) {
+  const cb_model_desc &m = c->m;
+  const int64_t rows = (int64_t)n_groups * n_seqs;
+  if (rows > (1 << 24) || rows * n_q > (1 << 24) || rows * n_q * m.n_q_heads > (1 << 28)) return false;
+  *a = SharedAttn();
+  a->dtype = m.dtype; a->hq = m.n_q_heads; a->hkv = m.n_kv_heads; a->dh = m.head_dim;
+  a->n_groups = n_groups; a->n_seqs = n_seqs; a->n_q = n_q; a->tail_stride = tail_stride;
+  shared_attention_plan(*a, max_ctx);
+  return true;
+}
+}  // namespace
+
+size_t cb_shared_prefix_workspace_bytes(const cb_ctx *c, int32_t n_groups, int32_t n_seqs, int32_t n_q, int32_t max_prefix,
+                                        int32_t tail_stride) {
+  if (!c || n_groups < 1 || n_seqs < 1 || n_q < 1 || max_prefix < 0 || tail_stride < 0) return 0;
+  SharedAttn a;
+  // what fewer groups, shorter contexts take is never more: the number of pieces falls with the length and the scratch is per row
+  if (!plan_shared(c, std::min(n_groups, kSharedGroups), n_seqs, n_q, max_prefix, tail_stride, &a)) return 0;
+  size_t floats = shared_attention_floats(a);
+  if (n_groups > kSharedGroups && n_groups % kSharedGroups) {          // the last launch has fewer groups, and so more pieces
+    plan_shared(c, n_groups % kSharedGroups, n_seqs, n_q, max_prefix, tail_stride, &a);
+    floats = std::max(floats, shared_attention_floats(a));
+  }
+  return align_up(std::max<size_t>(floats, 1) * 4, 256);
+}
+
+int cb_shared_prefix_attention(cb_ctx *c, const void *q, int32_t n_groups, int32_t n_seqs, int32_t n_q, const void *k_prefix,
+                               const void *v_prefix, const int32_t *prefix_lens, int32_t prefix_stride, const void *k_tail,
+                               const void *v_tail, int32_t tail_stride, const int32_t *row_tail, void *o, void *workspace,
+                               size_t workspace_bytes, void *stream) {
+  if (!c || !q || !prefix_lens || !row_tail || !o) return CB_ENULL;
+  if (n_groups < 1 || n_seqs < 1 || n_q < 1 || prefix_stride < 0 || tail_stride < 0) return CB_EINVAL;
+  int longest = 0;
+  for (int b = 0; b < n_groups; ++b) {
+    if (prefix_lens[b] < 0 || prefix_lens[b] > prefix_stride) return CB_EINVAL;
+    longest = std::max(longest, prefix_lens[b]);
+  }
+  if ((longest > 0 && (!k_prefix || !v_prefix)) || (tail_stride > 0 && (!k_tail || !v_tail)) || !workspace) return CB_ENULL;
+  if (!aligned(q, 16) || !aligned(k_prefix, 16) || !aligned(v_prefix, 16) || !aligned(k_tail, 16) || !aligned(v_tail, 16) ||
+      !aligned(row_tail, 4) || !aligned(o, 16) || !aligned(workspace, 256))
+    return CB_EINVAL;
+  SharedAttn a;
+  if (!plan_shared(c, std::min(n_groups, kSharedGroups), n_seqs, n_q, longest, tail_stride, &a)) return CB_EUNSUPPORTED;
+  if (workspace_bytes < cb_shared_prefix_workspace_bytes(c, n_groups, n_seqs, n_q, longest, tail_stride)) return CB_EWORKSPACE;
+  hipStream_t s = (hipStream_t)stream;
+  CB_TRY(check_stream(c, s));
+  const cb_model_desc &m = c->m;
+  const size_t es = esize(c), q_row = (size_t)m.n_q_heads * m.head_dim * es, kv_row = (size_t)m.n_kv_heads * m.head_dim * es;
+  double keys = 0, pairs = 0;
+  for (int b = 0; b < n_groups; ++b) {
+    keys += (double)prefix_lens[b] + (double)n_seqs * tail_stride;
+    pairs += (double)n_seqs * n_q * ((double)prefix_lens[b] + tail_stride);
+  }
+  ProfScope ps(c, s, CB_PROF_ATTN, 4.0 * m.n_q_heads * m.head_dim * pairs,
+               2.0 * keys * kv_row + 2.0 * (double)n_groups * n_seqs * n_q * q_row);
+  for (int g0 = 0; g0 < n_groups; g0 += kSharedGroups) {
+    const int ng = std::min(kSharedGroups, n_groups - g0);
+    if (g0 > 0) plan_shared(c, ng, n_seqs, n_q, longest, tail_stride, &a);
+    const size_t row0 = (size_t)g0 * n_seqs * n_q, slab0 = (size_t)g0 * n_seqs * tail_stride, ctx0 = (size_t)g0 * prefix_stride;
+    a.q = (const char *)q + row0 * q_row;
+    a.o = (char *)o + row0 * q_row;
+    a.row_tail = row_tail + row0;
+    a.kc = (const char *)k_prefix + ctx0 * kv_row;
+    a.vc = (const char *)v_prefix + ctx0 * kv_row;
+    a.kt = (const char *)k_tail + slab0 * kv_row;
+    a.vt = (const char *)v_tail + slab0 * kv_row;
+    a.ctx_stride = prefix_stride;
+    for (int b = 0; b < kSharedGroups; ++b) a.ctx_len[b] = b < ng ? prefix_lens[g0 + b] : 0;
+    CB_HIP(launch_shared_attention(a, (float *)workspace, s));
+  }
+  return CB_OK;
+}
+
+namespace {
+bool beam_shapes_ok(int32_t n_groups, int32_t n_beams, int32_t vocab, int32_t n_keep) {
+  return n_groups >= 1 && n_beams >= 1 && vocab >= 1 && n_keep >= 1;
+}
+bool beam_shapes_covered(int32_t n_groups, int32_t n_beams, int32_t vocab, int32_t n_keep) {
+  return n_beams <= kReorderBeams && n_keep <= kBeamKeep && (int64_t)n_groups * n_beams <= 65535 && vocab <= (1 << 30);
+}
+}  // namespace
+
+size_t cb_beam_select_workspace_bytes(const cb_ctx *c, int32_t n_groups, int32_t n_beams, int32_t vocab, int32_t n_keep) {
+  if (!c || !beam_shapes_ok(n_groups, n_beams, vocab, n_keep) || !beam_shapes_covered(n_groups, n_beams, vocab, n_keep)) return 0;
+  return beam_select_bytes(n_groups, n_beams, vocab, n_keep);
+}
+
+int cb_beam_select(cb_ctx *c, const void *logits, int32_t logits_dtype, int64_t row_stride, int32_t n_groups, int32_t n_beams,
+                   int32_t vocab, const float *scores, const int32_t *finished, int32_t end_token, int32_t n_keep, float *scores_out,
+                   int32_t *beam_out, int32_t *token_out, void *workspace, size_t workspace_bytes, void *stream) {
+  if (!c || !logits || !scores || !scores_out || !beam_out || !token_out || !workspace) return CB_ENULL;
+  if (!beam_shapes_ok(n_groups, n_beams, vocab, n_keep) || row_stride < vocab) return CB_EINVAL;
+  if (logits_dtype != CB_F32 && logits_dtype != CB_BF16) return CB_EINVAL;
+  if (finished && (end_token < 0 || end_token >= vocab)) return CB_EINVAL;
+  if (!aligned(logits, logits_dtype == CB_BF16 ? 2 : 4) || !aligned(scores, 4) || !aligned(finished, 4) || !aligned(scores_out, 4) ||
+      !aligned(beam_out, 4) || !aligned(token_out, 4) || !aligned(workspace, 256))
+    return CB_EINVAL;
+  if (!beam_shapes_covered(n_groups, n_beams, vocab, n_keep)) return CB_EUNSUPPORTED;
+  if (workspace_bytes < beam_select_bytes(n_groups, n_beams, vocab, n_keep)) return CB_EWORKSPACE;
+  hipStream_t s = (hipStream_t)stream;
+  CB_TRY(check_stream(c, s));
+  BeamSelect a = {logits, row_stride, logits_dtype, n_groups, n_beams, vocab, n_keep, end_token, scores, finished, scores_out, beam_out,
+                  token_out};
+  ProfScope ps(c, s, CB_PROF_HEAD, 0, (double)n_groups * n_beams * vocab * (logits_dtype == CB_BF16 ? 2 : 4));
+  CB_HIP(launch_beam_select(a, workspace, s));
+  return CB_OK;
+}
+
+int cb_beam_reorder(cb_ctx *c, void *const *k_tail_layers, void *const *v_tail_layers, int32_t layer_begin, int32_t layer_end,
+                    int32_t n_groups, int32_t n_beams, int32_t tail_stride, const int32_t *parent, const int32_t *seq_len, void *stream) {
+  if (!c || !k_tail_layers || !v_tail_layers || !parent) return CB_ENULL;
+  if (layer_begin < 0 || layer_end > c->m.n_layers || layer_begin > layer_end || n_groups < 1 || n_beams < 1 || tail_stride < 0)
+    return CB_EINVAL;
+  for (int l = layer_begin; l < layer_end; ++l) {
+    if (!k_tail_layers[l] || !v_tail_layers[l]) return CB_ENULL;
+    if (!aligned(k_tail_layers[l], 16) || !aligned(v_tail_layers[l], 16)) return CB_EINVAL;
+  }
+  if (!aligned(parent, 4) || !aligned(seq_len, 4)) return CB_EINVAL;
+  if (n_beams > kReorderBeams || n_groups > 65535) return CB_EUNSUPPORTED;
+  hipStream_t s = (hipStream_t)stream;
+  CB_TRY(check_stream(c, s));
+  if (layer_begin == layer_end || tail_stride == 0 || n_beams == 1) return CB_OK;
+  const int row_bytes = c->m.n_kv_heads * c->m.head_dim * (int)esize(c), nl = layer_end - layer_begin;
+  ProfScope ps(c, s, CB_PROF_OTHER, 0, 4.0 * nl * (double)n_groups * n_beams * tail_stride * row_bytes);
+  CB_HIP(launch_beam_reorder(k_tail_layers + layer_begin, v_tail_layers + layer_begin, nl, n_groups, n_beams, tail_stride, row_bytes,
+                             parent, seq_len, s));
   return CB_OK;
 }
 

@@ -157,4 +157,64 @@ long attention_query_workgroups(int n_rows, int n_q_heads, int n_kv_heads);
 hipError_t launch_lm_head(int dtype, const float *h_row, const void *gain, const void *w, int d, int vocab,
                           float eps, float *logits, int32_t *token, unsigned long long *pick, hipStream_t s);
 
+// ---- shared_attention.hip -----------------------------------------------------
+// Attention of n_groups x n_seqs continuations, n_q query rows each, over their group's context and their own tail:
+// row r (of continuation r / n_q) sees ctx_len[group] rows of its group's slab of kc / vc and the first row_tail[r] rows of its
+// continuation's slab of kt / vt; row_tail[r] < 0 marks a padding row, whose output is zero.
+constexpr int kSharedGroups = 64;          // groups per launch (their context lengths travel as arguments)
+struct SharedAttn {
+  const void *q, *kc, *vc, *kt, *vt;       // q, o: [rows, Hq, dh]; caches [*, Hkv, dh]
+  const int32_t *row_tail;                 // device
+  void *o;
+  int dtype, hq, hkv, dh;
+  int n_groups, n_seqs, n_q;
+  int ctx_stride, tail_stride;             // rows of a slab
+  int ctx_len[kSharedGroups];
+  // filled in by shared_attention_plan / launch_shared_attention
+  int rows, qb, ctx_blocks, ctx_pieces, ctx_items, tail_blocks, tail_pieces;
+  size_t tail_slot0;
+  float *part_o, *part_ml;
+  float scale_log2e;
+};
+// chooses the pieces for contexts of up to max_ctx rows (from the shapes above alone)
+void shared_attention_plan(SharedAttn &a, int max_ctx);
+// floats of scratch a planned launch needs
+size_t shared_attention_floats(const SharedAttn &a);
+hipError_t launch_shared_attention(SharedAttn a, float *scratch, hipStream_t s);
+
+// ---- beams.hip -------------------------------------------------------------------
+// q_out[r] = R(pos) (q[r] normalised), K cache row cache_row[r] = R(pos) (k[r] normalised), V cache row = v[r]; rows whose position
+// is outside the table are left out, rows whose cache_row is outside the cache are not stored.  Strides in elements.
+struct QkvRows {
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  const void *q_norm, *k_norm;             // gains [dh] (NULL: no norm)
+  const int32_t *row_pos, *cache_row;
+  void *q_out, *k_cache, *v_cache;
+  int64_t n_cache_rows;
+  const float2 *rope_tab;
+  int dtype, n_rows, hq, hkv, dh, rope_half, max_tokens;
+  float eps;
+};
+hipError_t launch_qkv_norm_rope(const QkvRows &a, hipStream_t s);
+
+// The n_keep best continuations of every group's n_beams rows of logits.
+constexpr int kBeamKeep = 64;              // most continuations kept per group
+struct BeamSelect {
+  const void *logits;
+  int64_t row_stride;                      // elements
+  int logits_dtype, n_groups, n_beams, vocab, n_keep, end_token;
+  const float *scores;                     // [n_groups * n_beams]
+  const int32_t *finished;                 // NULL or the same size
+  float *scores_out;                       // [n_groups * n_keep], as the next two
+  int32_t *beam_out, *token_out;
+};
+size_t beam_select_bytes(int n_groups, int n_beams, int vocab, int n_keep);
+hipError_t launch_beam_select(const BeamSelect &a, void *scratch, hipStream_t s);
+
+// Rows [0, seq_len[p]) of beam p = parent[b]'s slab become those of beam b, for all beams at once, in place, in every layer's arrays.
+constexpr int kReorderBeams = 64;
+hipError_t launch_beam_reorder(void *const *k_layers, void *const *v_layers, int n_layers, int n_groups, int n_beams, int tail_stride,
+                               int row_bytes, const int32_t *parent, const int32_t *seq_len, hipStream_t s);
+
 }  // namespace cb

@@ -1,0 +1,106 @@
+"""References of the operators that carry several continuations of one fused context, in 64 bits and from their definitions,
+with the error that the kernels' roundings can make of each output element."""
+import math
+from types import SimpleNamespace
+
+import torch
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF_STEP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}          # of a rounding, relative to the value
+
+
+def model(hq, hkv, dh, dtype, layers=1, rope="adjacent", theta=1e4):
+    return SimpleNamespace(n_layers=layers, d_model=hq * dh, n_q_heads=hq, n_kv_heads=hkv, head_dim=dh, d_ff=2 * hq * dh, rms_eps=1e-5,
+                           rope_theta=theta, dtype=dtype, rope_layout=rope)
+
+
+def normal(shape, seed, dtype=torch.float32, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return torch.empty(shape).normal_(0, std, generator=g).to(dtype)
+
+
+def attention(q, kp, vp, plen, kt, vt, row_tail, n_seqs, n_q, dtype):
+    """(out, bound) of cb_shared_prefix_attention, float64 on the inputs' device.  q [rows, Hq, dh]; kp [groups, stride, Hkv, dh];
+    kt [groups * n_seqs, stride, Hkv, dh].  The bound adds up, with A = sum p |v| and n keys:
+      - the probabilities' rounding to bf16 (A half steps; float models keep them) and the output's (|out| half steps);
+      - a score's float sum of dh products, dh 2^-24 of the sum of their magnitudes S, its scaling and the reduced exponent
+        (4 2^-24 of |score| <= S), on numerator and denominator: 2 A (dh + 4) 2^-24 max S;
+      - the sums over n keys, the exponentials (2 units of 2^-23), the rescaling and joining (8 more): 2 A (n + 24) 2^-24."""
+    rows, hq, dh = q.shape
+    hkv = kp.shape[2] if kp.numel() else kt.shape[2]
+    g = hq // hkv
+    out = torch.zeros(q.shape, dtype=torch.float64, device=q.device)
+    bound = torch.zeros_like(out)
+    for r in range(rows):
+        seq = r // n_q
+        group = seq // n_seqs
+        seen = int(row_tail[r])
+        if seen < 0:
+            continue
+        seen = min(seen, kt.shape[1])
+        k = torch.cat((kp[group, :plen[group]], kt[seq, :seen])).double()
+        v = torch.cat((vp[group, :plen[group]], vt[seq, :seen])).double()
+        n = k.shape[0]
+        if n == 0:
+            continue
+        qh = q[r].double().view(hkv, g, dh)
+        s = torch.einsum("hgd,nhd->hgn", qh, k) / math.sqrt(dh)
+        p = torch.softmax(s, -1)
+        out[r] = torch.einsum("hgn,nhd->hgd", p, v).reshape(hq, dh)
+        a = torch.einsum("hgn,nhd->hgd", p, v.abs()).reshape(hq, dh)
+        size = torch.einsum("hgd,nhd->hgn", qh.abs(), k.abs()).amax(-1).reshape(hq, 1) / math.sqrt(dh)
+        bound[r] = ((a if dtype == "bf16" else 0.0) + out[r].abs()) * HALF_STEP[dtype] * 1.01 + \
+            2 * a * ((dh + 4) * 2.0 ** -24 * size + (n + 24) * 2.0 ** -24)
+    return out, bound
+
+
+def rope(x, pos, gain, m):
+    """(out, bound) of the norm and rotation of x [rows, heads, dh] (gain None: no norm), float64.  Bound: the output's rounding, and for
+    the float arithmetic before it: the table's rounding 1, two products and a sum 3, the norm's factor (the sum's 8 levels, the
+    root 2, two products) 12: 16 units of 2^-24 of the magnitudes that are added."""
+    x = x.double()
+    half = m.head_dim // 2
+    if gain is not None:
+        x = x * torch.rsqrt(x.square().mean(-1, keepdim=True) + m.rms_eps) * gain.double()
+    inv = m.rope_theta ** (-2.0 * torch.arange(half, dtype=torch.float64, device=x.device) / m.head_dim)
+    ang = pos.double()[:, None, None] * inv
+    i = torch.arange(half, device=x.device)
+    a, b = (2 * i, 2 * i + 1) if m.rope_layout == "adjacent" else (i, i + half)
+    out, size = torch.empty_like(x), torch.empty_like(x)
+    out[..., a] = x[..., a] * ang.cos() - x[..., b] * ang.sin()
+    out[..., b] = x[..., a] * ang.sin() + x[..., b] * ang.cos()
+    size[..., a] = size[..., b] = x[..., a].abs() + x[..., b].abs()
+    return out, out.abs() * HALF_STEP[m.dtype] + size * 16 * 2.0 ** -24
+
+
+def beam_scores(logits, scores, finished=None, end_token=0):
+    """Scores of every continuation, float64 [rows, vocab], from the definition: NaN logits are -infinity, infinite ones share."""
+    x = logits.double().nan_to_num(nan=-math.inf, posinf=math.inf, neginf=-math.inf)
+    s = scores.double()
+    out = torch.full_like(x, -math.inf)
+    for r in range(x.shape[0]):
+        if finished is not None and int(finished[r]) != 0:
+            out[r, end_token] = s[r]
+            continue
+        m = float(x[r].max())
+        if m == -math.inf or torch.isnan(s[r]):
+            continue
+        if m == math.inf:
+            top = x[r] == math.inf
+            out[r, top] = s[r] - math.log(int(top.sum()))
+        else:
+            out[r] = s[r] + (x[r] - (m + torch.exp(x[r] - m).sum().log()))
+    return out.nan_to_num(nan=-math.inf, posinf=math.inf, neginf=-math.inf)
+
+
+def best(all_scores, n_groups, n_keep):
+    """(scores, beam, token) lists per group, best first; equal scores by lower beam, then lower token."""
+    rows, vocab = all_scores.shape
+    res = []
+    for g in range(n_groups):
+        flat = all_scores.view(n_groups, -1)[g]
+        v, i = torch.sort(flat, descending=True, stable=True)
+        v, i = v[:n_keep], i[:n_keep]
+        res.append([(float(a), int(b) // vocab, int(b) % vocab) if a > -math.inf else (-math.inf, -1, -1) for a, b in zip(v, i)] +
+                   [(-math.inf, -1, -1)] * (n_keep - len(v)))
+    return res
