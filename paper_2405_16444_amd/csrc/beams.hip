@@ -183,101 +183,158 @@ __global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScra
   for (int c = n + lane; c < K; c += 64) out[c] = 0;
 }
 
-// One workgroup per group: the rows' sums, then the best of all stretches' lists.
-struct Cand { double score; unsigned long long key; int beam; };
-__device__ __forceinline__ bool before(const Cand &a, const Cand &b) {      // a goes first
-  if (a.score != b.score) return a.score > b.score;
-  return a.beam != b.beam ? a.beam < b.beam : a.key > b.key;
-}
-
 // LDS written by some lanes of the wavefront is read by others
 __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
 
-constexpr int BF_CAP = 512;                // candidates held at a time
-__global__ __launch_bounds__(256) void beam_final_kernel(BeamSelect a, BeamScratch w) {
-  __shared__ double s_lse[kReorderBeams];
+// One workgroup per group: the rows' sums, then the best of all stretches' lists.  Its time is latency (a few dependent reads of
+// some KB), so little of the lists is looked at.  The D-th entries of the lists bound the result: where R of them, R D >= n_keep, are
+// at or before an entry, n_keep entries are; the R-th of the D-th entries, taken per wavefront, is such a bound, and only entries
+// at or before the tightest one are collected and ranked, as a rule one to three times n_keep.
+struct Cand { double score; unsigned long long key; int beam; };
+__device__ __forceinline__ bool before(const Cand &a, const Cand &b) {      // a goes first
+  if (a.score != b.score) return a.score > b.score;
+  return a.beam != b.beam ? a.beam < b.beam : a.key > b.key;
+}
+
+constexpr int BF_WAVES = 8;
+constexpr int BF_CAP = 1024;               // candidates collected at a time
+constexpr int BF_AHEAD = 4;                // entries of a list that are read before they are asked for
+__global__ __launch_bounds__(64 * BF_WAVES) void beam_final_kernel(BeamSelect a, BeamScratch w) {
+  __shared__ double s_lse[kReorderBeams], s_score[kReorderBeams];
   __shared__ int s_inf[kReorderBeams];     // the row's maximum is infinite
-  __shared__ Cand s_cand[BF_CAP], s_kept[kBeamKeep];
+  __shared__ Cand s_cand[BF_CAP], s_bound[BF_WAVES];
+  __shared__ int s_n;
+  constexpr int NT = 64 * BF_WAVES;
   const int grp = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int K = a.n_keep, B = a.n_beams;
-  for (int b = wave; b < B; b += 4) {
-    const int row = grp * B + b;
-    if (a.finished && a.finished[row] != 0) continue;
-    float m = -INFINITY;
-    for (int p = lane; p < w.pieces; p += 64) m = fmaxf(m, w.ms[(size_t)row * w.pieces + p].x);
-    m = wave_max(m);
-    double s = 0.0;
-    for (int p = lane; p < w.pieces; p += 64) {
-      const float2 v = w.ms[(size_t)row * w.pieces + p];
-      if (v.x == -INFINITY) continue;
-      s += m == INFINITY ? (v.x == INFINITY ? (double)v.y : 0.0) : (double)v.y * exp((double)v.x - (double)m);
-    }
+  const int K = a.n_keep, B = a.n_beams, lists = B * w.pieces;
+  auto ended = [&](int b) { return a.finished && a.finished[grp * B + b] != 0; };
+  // the first entries of the thread's first list are on their way while the sums are computed
+  unsigned long long ahead[BF_AHEAD] = {};
+  const int b0 = min(tid / w.pieces, B - 1);
+  const bool done0 = ended(b0);
+  const unsigned long long *list0 = w.keys + ((size_t)grp * lists + min(tid, lists - 1)) * K;
+  if (tid < lists && !done0) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    for (int i = 0; i < BF_AHEAD; ++i) ahead[i] = list0[min(i, K - 1)];
+  }
+  for (int b = wave; b < B; b += BF_WAVES) {
+    const float2 *ms = w.ms + ((size_t)grp * B + b) * w.pieces;
+    const bool done = ended(b);
+    float m = -INFINITY;
+    double s = 0.0;
+    if (!done) {
+      for (int p = lane; p < w.pieces; p += 64) m = fmaxf(m, ms[p].x);
+      m = wave_max(m);
+      for (int p = lane; p < w.pieces; p += 64) {
+        const float2 v = ms[p];
+        if (v.x > -INFINITY) s += m == INFINITY ? (v.x == INFINITY ? (double)v.y : 0.0) : (double)(v.y * expf(v.x - m));
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    }
     if (lane == 0) {
       s_lse[b] = (m == INFINITY ? 0.0 : (double)m) + log(s);
       s_inf[b] = m == INFINITY;
+      s_score[b] = (double)a.scores[grp * B + b];
     }
   }
+  if (tid == 0) s_n = 0;
   __syncthreads();
-  if (wave != 0) return;
-  // One wavefront takes one list per lane and step, and of every list its next entry as long as that can still be kept.
-  int n = 0;                               // candidates in s_cand
-  Cand worst = {-INFINITY, 0, B};          // once K are known: the last of the best K so far
-  auto rank_all = [&]() {                  // keeps the best K of s_cand, in order
-    for (int c0 = 0; c0 < n; c0 += 64) {
-      const bool has = c0 + lane < n;
-      const Cand mine = s_cand[has ? c0 + lane : 0];
-      int above = 0;
-      for (int c = 0; c < n; ++c) above += before(s_cand[c], mine);
-      if (has && above < K) s_kept[above] = mine;
-    }
-    wave_sync();
-    n = min(n, K);
-    for (int c = lane; c < n; c += 64) s_cand[c] = s_kept[c];
-    wave_sync();
-    if (n == K) worst = s_cand[K - 1];
-  };
-  const int lists = B * w.pieces;
-  for (int l0 = 0; l0 < lists; l0 += 64) {
-    const int l = l0 + lane, b = l / w.pieces, p = l - b * w.pieces, row = grp * B + min(b, B - 1);
-    const bool done = a.finished && a.finished[row] != 0;
-    const double s = (double)a.scores[row];
-    bool open = l < lists && !(done && p > 0);
-    const unsigned long long *keys = w.keys + ((size_t)row * w.pieces + p) * K;
-    for (int i = 0; i < K && __any(open); ++i) {
-      Cand c = {-INFINITY, 0, b};
-      if (open) {
-        if (done) {
-          c.score = s;
-          c.key = logit_key(0.f, a.end_token);
-          open = i == 0;
-        } else {
-          c.key = keys[i];
-          const float x = unord32((unsigned)(c.key >> 32));
-          c.score = s_inf[b] ? (x == INFINITY ? s - s_lse[b] : -INFINITY) : s + ((double)x - s_lse[b]);
-          open = c.key != 0;
-        }
-        open = open && c.score > -INFINITY && before(c, worst);      // NaN scores (of NaN beams) are left out, too
+  // entry i of list l; a score of -infinity where there is none (scores that are NaN are no continuations either)
+  auto entry = [&](int l, int i) {
+    Cand c = {-INFINITY, 0, l / w.pieces};
+    const double s = s_score[c.beam];
+    if (l == tid ? done0 : ended(c.beam)) {
+      if (i == 0 && l - c.beam * w.pieces == 0) {
+        c.key = logit_key(0.f, a.end_token);
+        c.score = s;
       }
-      const unsigned long long who = __ballot(open);
-      if (open) s_cand[n + __popcll(who & ((1ull << lane) - 1))] = c;
-      n += __popcll(who);
-      wave_sync();
-      if (n > BF_CAP - 64) rank_all();
-      if (done) open = false;
+    } else {
+      if (l == tid && i < BF_AHEAD) {
+#pragma unroll
+        for (int j = 0; j < BF_AHEAD; ++j)
+          if (j == i) c.key = ahead[j];
+      } else {
+        c.key = w.keys[((size_t)grp * lists + l) * K + i];
+      }
+      const float x = unord32((unsigned)(c.key >> 32));
+      if (c.key) c.score = s_inf[c.beam] ? (x == INFINITY ? s - s_lse[c.beam] : -INFINITY) : s + ((double)x - s_lse[c.beam]);
     }
-    rank_all();
+    if (!(c.score > -INFINITY)) c = {-INFINITY, 0, c.beam};
+    return c;
+  };
+  const Cand none = {-INFINITY, 0, 0x7FFFFFFF};
+  Cand bound = none;
+  {
+    const int in_wave = min(64, lists - wave * 64), D = in_wave > 0 ? min(K, max(1, 4 * K / in_wave)) : 1, R = (K + D - 1) / D;
+    Cand c = wave * 64 + lane < lists ? entry(wave * 64 + lane, D - 1) : none;
+    int rank = 0;
+    bool equal = false;
+    if (in_wave > 0) {
+#pragma unroll 8
+      for (int l = 0; l < 64; ++l) {
+        const double o = __longlong_as_double((long long)lane_value((unsigned long long)__double_as_longlong(c.score), l));
+        rank += o > c.score;
+        equal |= o == c.score && l != lane;
+      }
+      if (__any(equal && c.score > -INFINITY)) {
+        rank = 0;
+        for (int l = 0; l < 64; ++l) {
+          const Cand o = {__longlong_as_double((long long)lane_value((unsigned long long)__double_as_longlong(c.score), l)),
+                          lane_value(c.key, l), (int)__builtin_amdgcn_readlane((unsigned)c.beam, l)};
+          rank += before(o, c);
+        }
+      }
+    }
+    if (lane == 0) s_bound[wave] = none;
+    wave_sync();
+    if (rank == R - 1 && c.score > -INFINITY) s_bound[wave] = c;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < BF_WAVES; ++i)
+      if (before(s_bound[i], bound)) bound = s_bound[i];
   }
-  for (int c = lane; c < K; c += 64) {
-    const size_t o = (size_t)grp * K + c;
-    const bool has = c < n;
-    a.scores_out[o] = has ? (float)s_cand[has ? c : 0].score : -INFINITY;
-    a.beam_out[o] = has ? s_cand[has ? c : 0].beam : -1;
-    a.token_out[o] = has ? (int32_t)(0xFFFFFFFFu - (unsigned)s_cand[has ? c : 0].key) : -1;
+  int n;
+  for (;;) {
+    for (int l = tid; l < lists; l += NT)
+      for (int i = 0; i < K; ++i) {
+        const Cand c = entry(l, i);
+        if (!(c.score > -INFINITY) || before(bound, c)) break;
+        const int at = atomicAdd(&s_n, 1);                // where an entry lies does not matter: they are ranked below
+        if (at < BF_CAP) s_cand[at] = c;
+      }
+    __syncthreads();
+    n = s_n;
+    const int have = min(n, BF_CAP);
+    for (int i = tid; i < have; i += NT) {
+      const Cand c = s_cand[i];
+      int above = 0;
+      for (int j = 0; j < have; ++j) above += before(s_cand[j], c);
+      if (n <= BF_CAP) {
+        if (above < K) {
+          const size_t o = (size_t)grp * K + above;
+          a.scores_out[o] = (float)c.score;
+          a.beam_out[o] = c.beam;
+          a.token_out[o] = (int32_t)(0xFFFFFFFFu - (unsigned)c.key);
+        }
+      } else if (above == K - 1) {
+        s_bound[0] = c;                    // more than there is room for: the K-th of those at hand is a tighter bound (K < BF_CAP)
+      }
+    }
+    if (n <= BF_CAP) break;
+    __syncthreads();
+    bound = s_bound[0];
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+  }
+  for (int i = n + tid; i < K; i += NT) {
+    const size_t o = (size_t)grp * K + i;
+    a.scores_out[o] = -INFINITY;
+    a.beam_out[o] = -1;
+    a.token_out[o] = -1;
   }
 }
 
@@ -361,7 +418,7 @@ hipError_t launch_beam_select(const BeamSelect &a, void *scratch, hipStream_t s)
   else hipLaunchKernelGGL(beam_stretch_kernel<bf16>, grid, dim3(64), 0, s, a, w);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(beam_final_kernel, dim3(a.n_groups), dim3(256), 0, s, a, w);
+  hipLaunchKernelGGL(beam_final_kernel, dim3(a.n_groups), dim3(64 * BF_WAVES), 0, s, a, w);
   return hipGetLastError();
 }
 
