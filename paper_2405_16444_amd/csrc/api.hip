@@ -1084,12 +1084,11 @@ size_t cb_shared_prefix_workspace_bytes(const cb_ctx *c, int32_t n_groups, int32
                                         int32_t tail_stride) {
   if (!c || n_groups < 1 || n_seqs < 1 || n_q < 1 || max_prefix < 0 || tail_stride < 0) return 0;
   SharedAttn a;
-  // what fewer groups, shorter contexts take is never more: the number of pieces falls with the length and the scratch is per row
   if (!plan_shared(c, std::min(n_groups, kSharedGroups), n_seqs, n_q, max_prefix, tail_stride, &a)) return 0;
-  size_t floats = shared_attention_floats(a);
+  size_t floats = shared_attention_floats(a, max_prefix);
   if (n_groups > kSharedGroups && n_groups % kSharedGroups) {          // the last launch has fewer groups, and so more pieces
     plan_shared(c, n_groups % kSharedGroups, n_seqs, n_q, max_prefix, tail_stride, &a);
-    floats = std::max(floats, shared_attention_floats(a));
+    floats = std::max(floats, shared_attention_floats(a, max_prefix));
   }
   return align_up(std::max<size_t>(floats, 1) * 4, 256);
 }

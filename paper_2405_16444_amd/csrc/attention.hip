@@ -79,7 +79,9 @@ template <int V> struct IntC { static constexpr int value = V; };
 // tokens 644 -> 537 us, 500 rows over 3136 tokens 46 -> 40 us with the merge; a tile takes 1.42 us on an otherwise idle
 // chip (1.99 before) and 1.87 us with every CU busy, where power sets the clock.  The same loop on 16x16x32 MFMAs
 // measured 1.59 / 1.82 us, four wavefronts of 64 queries (half the LDS reads) did not fit the register file.
-template <int DH>
+// SHARED: the context part of attention over a context that several continuations share (shared_attention.hip).  Every query sees
+// cache rows 0 .. all_pos; q_pos marks padding rows by negative numbers, and partial results are left whatever the pieces.
+template <int DH, bool SHARED>
 __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__restrict__ q,
                                                         const int32_t *__restrict__ q_pos, int n_rows,
                                                         const bf16 *__restrict__ kc,
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__re
                                                         float *__restrict__ part_ml,
                                                         const int32_t *__restrict__ q_rows,
                                                         int32_t *__restrict__ wg_tiles,
-                                                        const int32_t *__restrict__ segs, int n_segs) {
+                                                        const int32_t *__restrict__ segs, int n_segs, int all_pos) {
   // K and V tiles sit row-major in LDS ([key][channel], no padding) and are filled by direct
   // global->LDS loads: one wavefront-wide 16-byte load writes 1 KB = RPI whole rows.  Instead of
   // padding, the 16-byte chunk c of row r is stored in slot c ^ f(r).
@@ -114,7 +116,7 @@ __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__re
   // Several requests in one launch: request s owns the query workgroups [segs[s].qwg, segs[s+1].qwg),
   // the rows [row0, row0 + rows) of q_pos / q_rows / o, and the cache rows from cache0 on.
   int seg_qwg0 = 0, row0 = 0;
-  if (segs) {
+  if (!SHARED && segs) {
     int lo = 0, hi = n_segs - 1;                       // last segment whose first workgroup is <= qwg
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -139,7 +141,8 @@ __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__re
   const int m_own = m_wg + wave * 32 + ln;
   const bool valid = m_own < n_flat;
   const int r_own = (valid ? m_own : n_flat - 1) / g, j_own = (valid ? m_own : n_flat - 1) - r_own * g;
-  const int my_pos = valid ? q_pos[r_own] : -1;
+  auto pos_of = [&](int r) { return SHARED ? (q_pos[r] < 0 ? -1 : all_pos) : q_pos[r]; };
+  const int my_pos = valid ? pos_of(r_own) : -1;
   const long q_off = ((long)(row0 + r_own) * n_q_heads + kvh * g + j_own) * DH;
   bf16x8 qf[NST];
   {
@@ -152,12 +155,12 @@ __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__re
   int max_pos = -1;
   {
     const int last_r = (min(m_wg + ATT_WGQ, n_flat) - 1) / g;
-    for (int r = m_wg / g + lane; r <= last_r; r += 64) max_pos = max(max_pos, q_pos[r]);
+    for (int r = m_wg / g + lane; r <= last_r; r += 64) max_pos = max(max_pos, pos_of(r));
   }
   const int kv_len = __builtin_amdgcn_readfirstlane(wave_max_i32(max_pos)) + 1;
   const int n_tiles_all = (kv_len + BKV - 1) / BKV;
   // the merge launch needs the same bound to know which pieces of the key range ran
-  if (gridDim.z > 1 && kvh == 0 && blockIdx.z == 0 && tid == 0) wg_tiles[qwg] = n_tiles_all;
+  if (!SHARED && gridDim.z > 1 && kvh == 0 && blockIdx.z == 0 && tid == 0) wg_tiles[qwg] = n_tiles_all;
   // KV split: workgroup z of gridDim.z handles tiles [t_begin, n_tiles) of the causal range and
   // leaves un-normalised partial results (flash-decoding style) for the merge kernel
   const int t_begin = blockIdx.z * split_tiles;
@@ -434,7 +437,7 @@ __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__re
     }
   }
   att_vm_wait<0>();                        // drain the clamped tail loads before the workgroup ends
-  if (gridDim.z > 1) {
+  if (SHARED || gridDim.z > 1) {
     // ---- partial results: O (un-normalised), reference and sum per (kv head, query, split) ----
     const float tot = row_sum + __shfl_xor(row_sum, 32, 64);
     if (!valid) return;
@@ -684,17 +687,12 @@ __global__ __launch_bounds__(64 * AF_NW) void attn_f32_kernel(const float *__res
 // range ends before that).  Measured on 359..986-row layers: about one round of 256 workgroups
 // in total is the optimum; more pieces cost more in partial results than they gain in balance.
 // n_qwg: query workgroups per kv head.
+static int attn_splits_wanted(long base, int max_tiles) {       // never falls with the number of tiles
+  if (base < 128) return std::min({(int)((256 + base - 1) / base), std::max(1, max_tiles / 4), 32});
+  return base < 256 ? std::min(2, std::max(1, max_tiles / 4)) : 1;
+}
 static void attn_split_plan(long n_qwg, int hkv, int n_tokens, int *n_splits, int *split_tiles) {
-  const long base = n_qwg * hkv;
-  const int max_tiles = (n_tokens + BKV - 1) / BKV;
-  int ns = 1;
-  if (base < 128) {
-    ns = (int)((256 + base - 1) / base);
-    ns = std::min(ns, std::max(1, max_tiles / 4));
-    ns = std::min(ns, 32);
-  } else if (base < 256) {
-    ns = std::min(2, std::max(1, max_tiles / 4));
-  }
+  const int max_tiles = (n_tokens + BKV - 1) / BKV, ns = attn_splits_wanted(n_qwg * hkv, max_tiles);
   *split_tiles = (max_tiles + ns - 1) / ns;
   *n_splits = (max_tiles + *split_tiles - 1) / *split_tiles;
 }
@@ -767,13 +765,13 @@ hipError_t launch_attention(int dtype, const void *q, const int32_t *q_rows, con
     constexpr int smem = 2 * ATT_S * BKV * DH_ * 2;                                                 \
     static std::once_flag once_;                                                                    \
     std::call_once(once_, [] {                                                                      \
-      (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_bf16_kernel<DH_>),             \
+      (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_bf16_kernel<DH_, false>),      \
                                 hipFuncAttributeMaxDynamicSharedMemorySize, smem);                  \
     });                                                                                             \
-    hipLaunchKernelGGL((attn_bf16_kernel<DH_>), dim3(hkv, (unsigned)n_qwg, n_splits),               \
+    hipLaunchKernelGGL((attn_bf16_kernel<DH_, false>), dim3(hkv, (unsigned)n_qwg, n_splits),        \
                        dim3(64 * ATT_NW), smem, s, (const bf16 *)q, q_pos, n_rows, (const bf16 *)kc, \
                        (const bf16 *)vc, (bf16 *)o, hq, hkv, scale_log2e, split_tiles, part_o,      \
-                       part_ml, q_rows, wg_tiles, segs, n_segs);                                    \
+                       part_ml, q_rows, wg_tiles, segs, n_segs, 0);                                 \
   } while (0)
   if (dh == 64) CB_ATTN(64);
   else CB_ATTN(128);
@@ -790,6 +788,34 @@ hipError_t launch_attention(int dtype, const void *q, const int32_t *q_rows, con
     hipLaunchKernelGGL(attn_merge_kernel<128>, mgrid, dim3(256), 0, s, part_o, part_ml, q_pos, n_rows,
                        (bf16 *)o, hq, hkv, n_splits, split_tiles, wgq, wg_tiles, n_flat_pad, segs, n_segs);
   return hipGetLastError();
+}
+
+void attention_context_plan(int n_rows, int hq, int hkv, int n_tokens, int *n_qwg, int *n_splits, int *split_tiles, int *most_splits) {
+  const long wg = query_workgroups(n_rows, hq, hkv);
+  *n_qwg = (int)wg;
+  attn_split_plan(wg, hkv, n_tokens, n_splits, split_tiles);
+  *most_splits = attn_splits_wanted(wg * hkv, (n_tokens + BKV - 1) / BKV);
+}
+
+template <int DH>
+static hipError_t launch_context(const bf16 *q, const int32_t *row_tail, int n_rows, const bf16 *kc, const bf16 *vc, int hq, int hkv, int n_ctx,
+                                 int n_qwg, int n_splits, int split_tiles, float *part_o, float *part_ml, hipStream_t s) {
+  constexpr int smem = 2 * ATT_S * BKV * DH * 2;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_bf16_kernel<DH, true>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+  });
+  hipLaunchKernelGGL((attn_bf16_kernel<DH, true>), dim3(hkv, n_qwg, n_splits), dim3(64 * ATT_NW), smem, s, q, row_tail, n_rows, kc, vc,
+                     (bf16 *)nullptr, hq, hkv, kLog2e / sqrtf((float)DH), split_tiles, part_o, part_ml, (const int32_t *)nullptr,
+                     (int32_t *)nullptr, (const int32_t *)nullptr, 0, n_ctx - 1);
+  return hipGetLastError();
+}
+hipError_t launch_attention_context(const void *q, const int32_t *row_tail, int n_rows, const void *kc, const void *vc, int hq, int hkv, int dh,
+                                    int n_ctx, int n_qwg, int n_splits, int split_tiles, float *part_o, float *part_ml, hipStream_t s) {
+  return dh == 64 ? launch_context<64>((const bf16 *)q, row_tail, n_rows, (const bf16 *)kc, (const bf16 *)vc, hq, hkv, n_ctx, n_qwg, n_splits,
+                                       split_tiles, part_o, part_ml, s)
+                  : launch_context<128>((const bf16 *)q, row_tail, n_rows, (const bf16 *)kc, (const bf16 *)vc, hq, hkv, n_ctx, n_qwg, n_splits,
+                                        split_tiles, part_o, part_ml, s);
 }
 
 }  // namespace cb

@@ -147,6 +147,14 @@ hipError_t launch_attention(int dtype, const void *q, const int32_t *q_rows, con
                             int n_kv_heads, int head_dim, int n_tokens, float *partial,
                             size_t partial_floats, hipStream_t s, const int32_t *segs = nullptr, int n_segs = 0,
                             long total_qwg = 0);
+// The context part of attention over a context that all queries see whole (bf16): un-normalised sums of row r's head j of key/value head
+// kvh over piece z in slot (kvh * n_qwg * 256 + r * g + j) * n_splits + z of part_o [slots][dh] and part_ml [slots][2] (maximum in
+// units of log2, sum of exponentials), for the pieces z < ceil(tiles of 64 keys / split_tiles).  Rows with row_tail[r] < 0 are
+// padding, whose slots may be left as they are.  n_ctx >= 1.  most_splits: no context of up to n_tokens rows takes more pieces.
+void attention_context_plan(int n_rows, int hq, int hkv, int n_tokens, int *n_qwg, int *n_splits, int *split_tiles,
+                            int *most_splits);
+hipError_t launch_attention_context(const void *q, const int32_t *row_tail, int n_rows, const void *kc, const void *vc, int hq, int hkv, int dh,
+                                    int n_ctx, int n_qwg, int n_splits, int split_tiles, float *part_o, float *part_ml, hipStream_t s);
 // query workgroups (per kv head) a request with n_rows rows occupies in the bf16 kernel's grid
 long attention_query_workgroups(int n_rows, int n_q_heads, int n_kv_heads);
 
@@ -161,25 +169,39 @@ hipError_t launch_lm_head(int dtype, const float *h_row, const void *gain, const
 // Attention of n_groups x n_seqs continuations, n_q query rows each, over their group's context and their own tail:
 // row r (of continuation r / n_q) sees ctx_len[group] rows of its group's slab of kc / vc and the first row_tail[r] rows of its
 // continuation's slab of kt / vt; row_tail[r] < 0 marks a padding row, whose output is zero.
+// n / d by a multiplication: m = 2^32 / d rounded down (d = 1: 2^32 - 1) gives a quotient at most one too small for n < 2^31
+struct FastDiv {
+  unsigned d, m;
+  FastDiv(unsigned div = 1) : d(div), m(div == 1 ? 0xFFFFFFFFu : (unsigned)((1ull << 32) / div)) {}
+  __host__ __device__ unsigned div(unsigned n) const {
+    const unsigned q = (unsigned)(((unsigned long long)n * m) >> 32);
+    return q + (n - q * d >= d);
+  }
+};
 constexpr int kSharedGroups = 64;          // groups per launch (their context lengths travel as arguments)
 struct SharedAttn {
   const void *q, *kc, *vc, *kt, *vt;       // q, o: [rows, Hq, dh]; caches [*, Hkv, dh]
   const int32_t *row_tail;                 // device
-  void *o;
-  int dtype, hq, hkv, dh;
-  int n_groups, n_seqs, n_q;
+  // filled in by shared_attention_plan / launch_shared_attention
+  float *part_o, *part_ml;
+  size_t tail_slot0;
+  FastDiv by_hkv, by_g, by_ctx_pieces, by_ctx_blocks, by_tail_pieces, by_tail_blocks;
+  int rows, g, ctx_items;
+  float scale_log2e;
+  // shapes
+  int hq, hkv, dh, n_groups, n_seqs, n_q;
   int ctx_stride, tail_stride;             // rows of a slab
   int ctx_len[kSharedGroups];
-  // filled in by shared_attention_plan / launch_shared_attention
-  int rows, qb, ctx_blocks, ctx_pieces, ctx_items, tail_blocks, tail_pieces;
-  size_t tail_slot0;
-  float *part_o, *part_ml;
-  float scale_log2e;
+  void *o;
+  int dtype, qb, ctx_blocks, ctx_pieces, tail_blocks, tail_pieces;
+  // wide: a launch of its own for the context (attention_context_plan); ctx_rows: queries of a group in its slots' numbering
+  int wide, n_qwg, split_tiles, ctx_rows, most_pieces;
+  FastDiv by_group_rows, by_hq;
 };
 // chooses the pieces for contexts of up to max_ctx rows (from the shapes above alone)
 void shared_attention_plan(SharedAttn &a, int max_ctx);
-// floats of scratch a planned launch needs
-size_t shared_attention_floats(const SharedAttn &a);
+// floats of scratch that launches with contexts of up to max_ctx rows need; never falls with max_ctx
+size_t shared_attention_floats(SharedAttn a, int max_ctx);
 hipError_t launch_shared_attention(SharedAttn a, float *scratch, hipStream_t s);
 
 // ---- beams.hip -------------------------------------------------------------------
