@@ -83,8 +83,8 @@ __global__ __launch_bounds__(256) void qkv_norm_rope_kernel(QkvRows a) {
 // the best of every stretch of a row without knowing its sum; it reads every logit once.  Scores are compared in double:
 // two beams' scores are seldom closer than 1e-7 of each other, the float resolution, but they are not never.
 // ---------------------------------------------------------------------------
-constexpr int BS_PER = 32;                 // logits per lane
-constexpr int BS_PIECE = 64 * BS_PER;      // logits per wavefront
+constexpr int BS_PER = 32;                 // logits per lane and round
+constexpr int BS_CAP = 256;                // candidates a wavefront holds
 
 // larger logit, then lower token <=> larger key; 0 is below every key (logits are neither NaN nor -infinity)
 __device__ __forceinline__ unsigned ord32(float v) {
@@ -103,85 +103,9 @@ __device__ __forceinline__ unsigned long long lane_value(unsigned long long v, i
 struct BeamScratch {
   float2 *ms;                              // [rows][pieces] maximum and sum of exponentials of a stretch
   unsigned long long *keys;                // [rows][pieces][n_keep] its best logits, descending, 0 behind the last
-  int pieces;
+  FastDiv by_lists, by_beams;              // lists of a group, beams of a group
+  int pieces, rounds;                      // stretches of a row, each rounds * 64 * BS_PER logits
 };
-
-// One wavefront: a stretch of BS_PIECE logits.  What can be among its n_keep best lies in the n_keep lanes with the largest
-// maxima, at or above the n_keep-th largest of them: that threshold leaves little more than n_keep logits to be ranked.
-template <typename TL>
-__global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScratch w) {
-  using V = Vec16<TL>;
-  constexpr int N = V::N, NV = BS_PER / N;
-  __shared__ unsigned long long s_list[BS_PIECE];
-  const int row = blockIdx.y, piece = blockIdx.x, lane = threadIdx.x;
-  if (a.finished && a.finished[row] != 0) return;
-  const TL *src = (const TL *)a.logits + (size_t)row * a.row_stride;
-  const int t0 = piece * BS_PIECE;
-  const int K = a.n_keep;
-  float x[BS_PER];
-  int tok[NV];
-  // 16-byte loads where the row's address allows them, single elements otherwise
-  const bool wide = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int t = t0 + (i * 64 + lane) * N;
-    tok[i] = t;
-    if (wide && t + N <= a.vocab) {
-      const V v = *reinterpret_cast<const V *>(src + t);
-#pragma unroll
-      for (int j = 0; j < N; ++j) x[i * N + j] = v.get(j);
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) x[i * N + j] = t + j < a.vocab ? to_f32(src[t + j]) : -INFINITY;
-    }
-  }
-  float m = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < BS_PER; ++i) {
-    x[i] = x[i] == x[i] ? x[i] : -INFINITY;              // a NaN logit counts as -infinity
-    m = fmaxf(m, x[i]);
-  }
-  unsigned long long best = 0;                           // the lane's best key: its first logit that equals the maximum
-#pragma unroll
-  for (int i = BS_PER - 1; i >= 0; --i)
-    if (x[i] == m) best = logit_key(m, tok[i / N] + i % N);
-  const float wm = wave_max(m);
-  // sum of the exponentials; with an infinite maximum the infinite logits share the probability
-  float sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < BS_PER; ++i) sum += wm == INFINITY ? (x[i] == INFINITY ? 1.f : 0.f) : wm == -INFINITY ? 0.f : expf(x[i] - wm);
-  sum = wave_sum(sum);
-  const size_t at = (size_t)row * w.pieces + piece;
-  if (lane == 0) w.ms[at] = make_float2(wm, sum);
-  // threshold: the K-th largest of the lanes' best keys (0 where fewer lanes have any)
-  int rank = 0;
-#pragma unroll 8
-  for (int l = 0; l < 64; ++l) rank += lane_value(best, l) > best;
-  unsigned long long thr = 0;
-  const unsigned long long kth = __ballot(rank == K - 1 && best != 0);
-  if (kth) thr = lane_value(best, __ffsll((long long)kth) - 1);
-  const float tv = thr ? unord32((unsigned)(thr >> 32)) : -INFINITY;
-  int n = 0;
-#pragma unroll
-  for (int i = 0; i < BS_PER; ++i) {
-    const unsigned long long key = logit_key(x[i], tok[i / N] + i % N);
-    const bool in = x[i] >= tv && key >= thr && key != 0;
-    const unsigned long long who = __ballot(in);
-    if (who) {
-      if (in) s_list[n + __popcll(who & ((1ull << lane) - 1))] = key;
-      n += __popcll(who);
-    }
-  }
-  __syncthreads();
-  unsigned long long *out = w.keys + at * K;
-  for (int c0 = 0; c0 < n; c0 += 64) {
-    const unsigned long long mine = c0 + lane < n ? s_list[c0 + lane] : 0ull;
-    int above = 0;
-    for (int c = 0; c < n; ++c) above += s_list[c] > mine;
-    if (mine && above < K) out[above] = mine;
-  }
-  for (int c = n + lane; c < K; c += 64) out[c] = 0;
-}
 
 // LDS written by some lanes of the wavefront is read by others
 __device__ __forceinline__ void wave_sync() {
@@ -189,158 +113,332 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// One workgroup per group: the rows' sums, then the best of all stretches' lists.  Its time is latency (a few dependent reads of
-// some KB), so little of the lists is looked at.  The D-th entries of the lists bound the result: where R of them, R D >= n_keep, are
-// at or before an entry, n_keep entries are; the R-th of the D-th entries, taken per wavefront, is such a bound, and only entries
-// at or before the tightest one are collected and ranked, as a rule one to three times n_keep.
-struct Cand { double score; unsigned long long key; int beam; };
-__device__ __forceinline__ bool before(const Cand &a, const Cand &b) {      // a goes first
-  if (a.score != b.score) return a.score > b.score;
-  return a.beam != b.beam ? a.beam < b.beam : a.key > b.key;
+// One wavefront: a stretch of a row, 64 x BS_PER logits at a time, the next ones on their way meanwhile.  Bound by HBM where there are many
+// rows, so the instructions per logit count: the running maximum and sum of exponentials, kept per lane and joined at the end
+// (a subtraction, a product, an exponential, an addition), and one comparison with the threshold.  The threshold comes from the first
+// round: what can be among the n_keep best lies in the n_keep lanes with the largest maxima, at or above the
+// n_keep-th largest of them.  What passes it goes to a list that is ranked at the end, or when it is half full, which
+// tightens the threshold; where it overflows (many equal logits), the n_keep-th of those at hand does, and the round is gone through again.
+template <typename TL>
+__global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScratch w) {
+  using V = Vec16<TL>;
+  constexpr int N = V::N, NV = BS_PER / N;
+  constexpr float kLog2e = 1.4426950408889634f;
+  __shared__ unsigned long long s_list[BS_CAP];
+  const int row = blockIdx.y, piece = blockIdx.x, lane = threadIdx.x, K = a.n_keep;
+  if (a.finished && a.finished[row] != 0) return;
+  const TL *src = (const TL *)a.logits + (size_t)row * a.row_stride;
+  // Which lane adds up which tokens depends on the tokens alone, so that equal rows have equal sums wherever they start: 16-byte loads at any
+  // alignment of the type (the hardware takes them), the last vector of a row element by element.
+  const int t0 = piece * w.rounds * (64 * BS_PER) + lane * N;
+  V raw[NV];
+  auto load = [&](int round) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int t = t0 + (round * NV + i) * 64 * N;
+      if (t + N <= a.vocab) {
+        __builtin_memcpy(&raw[i], src + t, sizeof(V));
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) raw[i].set(j, t + j < a.vocab ? to_f32(src[t + j]) : -INFINITY);
+      }
+    }
+  };
+  load(0);
+  float lm = -INFINITY, ls = 0.f, tv = -INFINITY;
+  unsigned long long thr = 0;
+  int n = 0;
+#pragma unroll 1
+  for (int round = 0; round < w.rounds; ++round) {
+    float x[BS_PER];
+#pragma unroll
+    for (int i = 0; i < BS_PER; ++i) x[i] = fmaxf(raw[i / N].get(i % N), -INFINITY);      // NaN counts as -infinity
+    if (round + 1 < w.rounds) load(round + 1);
+    const int tr = t0 + round * 64 * BS_PER;
+    auto token = [&](int i) { return tr + i / N * 64 * N + i % N; };
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < BS_PER; ++i) m = fmaxf(m, x[i]);
+    const float nm = fmaxf(lm, m);
+    if (__any(nm == INFINITY)) {           // infinite logits share the probability: the sum is their number
+      ls = nm == INFINITY && lm == INFINITY ? ls : nm == INFINITY ? 0.f : ls * __builtin_amdgcn_exp2f((lm - (nm == -INFINITY ? 0.f : nm)) * kLog2e);
+#pragma unroll
+      for (int i = 0; i < BS_PER; ++i)
+        ls += nm == INFINITY ? (x[i] == INFINITY ? 1.f : 0.f) : nm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i] - nm) * kLog2e);
+    } else {
+      const float base = nm == -INFINITY ? 0.f : nm;
+      ls *= __builtin_amdgcn_exp2f((lm - base) * kLog2e);
+      float part = 0.f;
+#pragma unroll
+      for (int i = 0; i < BS_PER; ++i) part += __builtin_amdgcn_exp2f((x[i] - base) * kLog2e);
+      ls += part;
+    }
+    lm = nm;
+    if (round == 0) {
+      unsigned long long best = 0;         // the lane's best key: the lowest of its tokens with the maximum
+#pragma unroll
+      for (int i = BS_PER - 1; i >= 0; --i)
+        if (x[i] == m) best = logit_key(m, token(i));
+      int rank = 0;
+#pragma unroll 8
+      for (int l = 0; l < 64; ++l) rank += lane_value(best, l) > best;
+      const unsigned long long kth = __ballot(rank == K - 1 && best != 0);
+      if (kth) {
+        thr = lane_value(best, __ffsll((long long)kth) - 1);
+        tv = unord32((unsigned)(thr >> 32));
+      }
+    }
+    const int kept = n;
+    const bool last = round + 1 == w.rounds;
+    bool over = __any(m >= tv) || last;
+    while (over) {
+      n = kept;
+#pragma unroll
+      for (int i = 0; i < BS_PER; ++i) {
+        if (__any(x[i] >= tv)) {
+          const unsigned long long key = logit_key(x[i], token(i));
+          const bool in = key != 0 && key >= thr;
+          const unsigned long long who = __ballot(in);
+          const int at = n + __popcll(who & ((1ull << lane) - 1));
+          if (in && at < BS_CAP) s_list[at] = key;
+          n += __popcll(who);
+        }
+      }
+      over = n > BS_CAP;
+      if (!over && !last && n <= BS_CAP / 2) break;
+      // rank what is at hand, four entries per lane
+      wave_sync();
+      const int have = min(n, BS_CAP);
+      unsigned long long mine[BS_CAP / 64];
+      int above[BS_CAP / 64];
+#pragma unroll
+      for (int j = 0; j < BS_CAP / 64; ++j) {
+        mine[j] = j * 64 + lane < have ? s_list[j * 64 + lane] : 0;
+        above[j] = mine[j] ? 0 : BS_CAP;
+      }
+      if (have <= 64) {
+#pragma unroll 8
+        for (int c = 0; c < have; ++c) above[0] += s_list[c] > mine[0];
+      } else {
+#pragma unroll 4
+        for (int c = 0; c < have; ++c) {
+          const unsigned long long k = s_list[c];
+#pragma unroll
+          for (int j = 0; j < BS_CAP / 64; ++j) above[j] += k > mine[j];
+        }
+      }
+      wave_sync();
+      if (!over) n = min(have, K);
+#pragma unroll
+      for (int j = 0; j < BS_CAP / 64; ++j) {
+        if (!over && above[j] < K) s_list[above[j]] = mine[j];
+        const unsigned long long kth = __ballot(above[j] == K - 1);
+        if (kth) thr = lane_value(mine[j], __ffsll((long long)kth) - 1);
+      }
+      if (thr) tv = unord32((unsigned)(thr >> 32));
+      wave_sync();
+    }
+  }
+  const float wm = wave_max(lm);
+  // a lane whose maximum is not the infinite one of the row adds nothing to it
+  float sum = wm == INFINITY ? (lm == INFINITY ? ls : 0.f) : wm == -INFINITY ? 0.f : ls * __builtin_amdgcn_exp2f((lm - wm) * kLog2e);
+  sum = wave_sum(sum);
+  const size_t at = (size_t)row * w.pieces + piece;
+  if (lane == 0) w.ms[at] = make_float2(wm, sum);
+  if (lane < K) w.keys[at * K + lane] = lane < n ? s_list[lane] : 0;
 }
 
-constexpr int BF_WAVES = 8;
-constexpr int BF_CAP = 1024;               // candidates collected at a time
-constexpr int BF_AHEAD = 4;                // entries of a list that are read before they are asked for
-__global__ __launch_bounds__(64 * BF_WAVES) void beam_final_kernel(BeamSelect a, BeamScratch w) {
+// One workgroup per group: the rows' sums, then the best of all stretches' lists.  Its time is latency, so there are few dependent steps: a
+// thread reads its share of the lists' entries while the sums are computed, 64 groups of threads take the maxima of theirs, the
+// n_keep-th largest of these is at or below n_keep entries and so a bound, and what reaches it (as a rule one to four times n_keep) is ranked by
+// counting, several threads to an entry.  Entries are numbered by depth in their list, then stretch, then beam, so that each
+// group of threads sees every beam.
+struct Cand { unsigned long long score, key; int beam; };      // score: order-preserving image of the double
+__device__ __forceinline__ unsigned long long ord64(double v) {
+  const unsigned long long u = (unsigned long long)__double_as_longlong(v + 0.0);
+  return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+__device__ __forceinline__ double unord64(unsigned long long o) {
+  return __longlong_as_double((long long)(o >> 63 ? o & 0x7FFFFFFFFFFFFFFFull : ~o));
+}
+__device__ __forceinline__ bool before(const Cand &a, const Cand &b) {      // a goes first
+  const bool tie = a.beam < b.beam || (a.beam == b.beam && a.key > b.key);
+  return a.score > b.score || (a.score == b.score && tie);
+}
+__device__ __forceinline__ unsigned long long max64(unsigned long long a, unsigned long long b) { return a > b ? a : b; }
+
+constexpr int BF_WAVES = 8, BF_THREADS = 64 * BF_WAVES;
+constexpr int BF_PER = 8;                  // entries per thread and batch
+constexpr int BF_CAP = 1024;               // candidates held, those kept from batches before among them
+__global__ __launch_bounds__(BF_THREADS) void beam_final_kernel(BeamSelect a, BeamScratch w) {
   __shared__ double s_lse[kReorderBeams], s_score[kReorderBeams];
-  __shared__ int s_inf[kReorderBeams];     // the row's maximum is infinite
-  __shared__ Cand s_cand[BF_CAP], s_bound[BF_WAVES];
-  __shared__ int s_n;
-  constexpr int NT = 64 * BF_WAVES;
+  __shared__ int s_state[kReorderBeams];   // 1: the row's maximum is infinite, 2: the beam has ended
+  __shared__ unsigned long long s_so[BF_CAP], s_key[BF_CAP], s_max[64], s_keep_so[kBeamKeep], s_keep_key[kBeamKeep];
+  __shared__ int s_beam[BF_CAP], s_keep_beam[kBeamKeep], s_n;
   const int grp = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int K = a.n_keep, B = a.n_beams, lists = B * w.pieces;
-  auto ended = [&](int b) { return a.finished && a.finished[grp * B + b] != 0; };
-  // the first entries of the thread's first list are on their way while the sums are computed
-  unsigned long long ahead[BF_AHEAD] = {};
-  const int b0 = min(tid / w.pieces, B - 1);
-  const bool done0 = ended(b0);
-  const unsigned long long *list0 = w.keys + ((size_t)grp * lists + min(tid, lists - 1)) * K;
-  if (tid < lists && !done0) {
+  const int K = a.n_keep, B = a.n_beams;
+  const unsigned lists = B * w.pieces;
+  const long entries = (long)lists * K;
+  unsigned long long key[BF_PER];
+  int beam[BF_PER];
+  auto fetch = [&](long e0) {
 #pragma unroll
-    for (int i = 0; i < BF_AHEAD; ++i) ahead[i] = list0[min(i, K - 1)];
-  }
-  for (int b = wave; b < B; b += BF_WAVES) {
-    const float2 *ms = w.ms + ((size_t)grp * B + b) * w.pieces;
-    const bool done = ended(b);
-    float m = -INFINITY;
-    double s = 0.0;
-    if (!done) {
-      for (int p = lane; p < w.pieces; p += 64) m = fmaxf(m, ms[p].x);
-      m = wave_max(m);
-      for (int p = lane; p < w.pieces; p += 64) {
-        const float2 v = ms[p];
-        if (v.x > -INFINITY) s += m == INFINITY ? (v.x == INFINITY ? (double)v.y : 0.0) : (double)(v.y * expf(v.x - m));
+    for (int j = 0; j < BF_PER; ++j) {
+      const long e = e0 + j * BF_THREADS + tid;
+      key[j] = 0;
+      beam[j] = 0;
+      if (e0 + j * BF_THREADS < entries) {               // the same for all threads
+        const unsigned ec = (unsigned)(e < entries ? e : entries - 1), depth = w.by_lists.div(ec), l = ec - depth * lists, p = w.by_beams.div(l);
+        beam[j] = e < entries ? (int)(l - p * B) : -1;
+        key[j] = w.keys[(((size_t)grp * B + (l - p * B)) * w.pieces + p) * K + depth];
+        if (p == 0 && depth == 0) beam[j] |= 0x10000;    // the entry that stands for a beam that has ended
       }
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     }
+  };
+  fetch(0);
+  for (int b = wave; b < B; b += BF_WAVES) {
+    const int row = grp * B + b;
+    const float2 *ms = w.ms + (size_t)row * w.pieces;
+    float2 v = lane < w.pieces ? ms[lane] : make_float2(-INFINITY, 0.f);
+    const bool done = a.finished && a.finished[row] != 0;
+    const float score = a.scores[row];
+    float m = v.x, s = 0.f;
+    for (int p = 64 + lane; p < w.pieces; p += 64) m = fmaxf(m, ms[p].x);
+    m = wave_max(m);
+    const float base = fabsf(m) < INFINITY ? m : 0.f;
+    for (int p = lane;; v = ms[p]) {
+      if (v.x > -INFINITY) s += m == INFINITY ? (v.x == INFINITY ? v.y : 0.f) : v.y * expf(v.x - base);
+      if ((p += 64) >= w.pieces) break;
+    }
+    s = wave_sum(s);
     if (lane == 0) {
-      s_lse[b] = (m == INFINITY ? 0.0 : (double)m) + log(s);
-      s_inf[b] = m == INFINITY;
-      s_score[b] = (double)a.scores[grp * B + b];
+      s_lse[b] = (double)base + log((double)s);
+      s_state[b] = done ? 2 : m == INFINITY;
+      s_score[b] = (double)score;
     }
   }
   if (tid == 0) s_n = 0;
   __syncthreads();
-  // entry i of list l; a score of -infinity where there is none (scores that are NaN are no continuations either)
-  auto entry = [&](int l, int i) {
-    Cand c = {-INFINITY, 0, l / w.pieces};
-    const double s = s_score[c.beam];
-    if (l == tid ? done0 : ended(c.beam)) {
-      if (i == 0 && l - c.beam * w.pieces == 0) {
-        c.key = logit_key(0.f, a.end_token);
-        c.score = s;
-      }
-    } else {
-      if (l == tid && i < BF_AHEAD) {
+  unsigned long long kth = 0;              // score of the n_keep-th best of the batches so far
+  int kept = 0;
+  for (long e0 = 0; e0 < entries; e0 += BF_THREADS * BF_PER) {
+    if (e0 > 0) fetch(e0);
+    unsigned long long so[BF_PER], best = 0;
 #pragma unroll
-        for (int j = 0; j < BF_AHEAD; ++j)
-          if (j == i) c.key = ahead[j];
-      } else {
-        c.key = w.keys[((size_t)grp * lists + l) * K + i];
+    for (int j = 0; j < BF_PER; ++j) {
+      so[j] = 0;                           // no continuation (also one whose score would be -infinity or NaN)
+      if (e0 + j * BF_THREADS < entries) {
+        const bool first = beam[j] >= 0 && (beam[j] & 0x10000);
+        const bool real = beam[j] >= 0;
+        beam[j] &= 0xFFFF;
+        const int b = real ? beam[j] : 0, state = s_state[b];
+        const float x = unord32((unsigned)(key[j] >> 32));
+        double score = s_score[b] + ((state == 1 ? 0.0 : (double)x) - s_lse[b]);
+        bool in = real && key[j] != 0 && (state == 0 || (state == 1 && x == INFINITY));
+        if (state == 2) {
+          in = real && first;
+          score = s_score[b];
+          key[j] = logit_key(0.f, a.end_token);
+        }
+        if (in && score > -INFINITY) so[j] = ord64(score);
+        best = max64(best, so[j]);
       }
-      const float x = unord32((unsigned)(c.key >> 32));
-      if (c.key) c.score = s_inf[c.beam] ? (x == INFINITY ? s - s_lse[c.beam] : -INFINITY) : s + ((double)x - s_lse[c.beam]);
     }
-    if (!(c.score > -INFINITY)) c = {-INFINITY, 0, c.beam};
-    return c;
-  };
-  const Cand none = {-INFINITY, 0, 0x7FFFFFFF};
-  Cand bound = none;
-  {
-    const int in_wave = min(64, lists - wave * 64), D = in_wave > 0 ? min(K, max(1, 4 * K / in_wave)) : 1, R = (K + D - 1) / D;
-    Cand c = wave * 64 + lane < lists ? entry(wave * 64 + lane, D - 1) : none;
-    int rank = 0;
-    bool equal = false;
-    if (in_wave > 0) {
+#pragma unroll
+    for (int o = 1; o < BF_THREADS / 64; o <<= 1) best = max64(best, (unsigned long long)__shfl_xor((long long)best, o, 64));
+    if (tid % (BF_THREADS / 64) == 0) s_max[tid / (BF_THREADS / 64)] = best;
+    __syncthreads();
+    {
+      const unsigned long long mine = s_max[lane];
+      int at_least = 0;
 #pragma unroll 8
-      for (int l = 0; l < 64; ++l) {
-        const double o = __longlong_as_double((long long)lane_value((unsigned long long)__double_as_longlong(c.score), l));
-        rank += o > c.score;
-        equal |= o == c.score && l != lane;
-      }
-      if (__any(equal && c.score > -INFINITY)) {
-        rank = 0;
-        for (int l = 0; l < 64; ++l) {
-          const Cand o = {__longlong_as_double((long long)lane_value((unsigned long long)__double_as_longlong(c.score), l)),
-                          lane_value(c.key, l), (int)__builtin_amdgcn_readlane((unsigned)c.beam, l)};
-          rank += before(o, c);
-        }
-      }
-    }
-    if (lane == 0) s_bound[wave] = none;
-    wave_sync();
-    if (rank == R - 1 && c.score > -INFINITY) s_bound[wave] = c;
-    __syncthreads();
+      for (int i = 0; i < 64; ++i) at_least += s_max[i] >= mine;
+      unsigned long long c = at_least >= K ? mine : 0;
 #pragma unroll
-    for (int i = 0; i < BF_WAVES; ++i)
-      if (before(s_bound[i], bound)) bound = s_bound[i];
-  }
-  int n;
-  for (;;) {
-    for (int l = tid; l < lists; l += NT)
-      for (int i = 0; i < K; ++i) {
-        const Cand c = entry(l, i);
-        if (!(c.score > -INFINITY) || before(bound, c)) break;
-        const int at = atomicAdd(&s_n, 1);                // where an entry lies does not matter: they are ranked below
-        if (at < BF_CAP) s_cand[at] = c;
-      }
-    __syncthreads();
-    n = s_n;
-    const int have = min(n, BF_CAP);
-    for (int i = tid; i < have; i += NT) {
-      const Cand c = s_cand[i];
-      int above = 0;
-      for (int j = 0; j < have; ++j) above += before(s_cand[j], c);
-      if (n <= BF_CAP) {
-        if (above < K) {
-          const size_t o = (size_t)grp * K + above;
-          a.scores_out[o] = (float)c.score;
-          a.beam_out[o] = c.beam;
-          a.token_out[o] = (int32_t)(0xFFFFFFFFu - (unsigned)c.key);
-        }
-      } else if (above == K - 1) {
-        s_bound[0] = c;                    // more than there is room for: the K-th of those at hand is a tighter bound (K < BF_CAP)
-      }
+      for (int o = 32; o > 0; o >>= 1) c = max64(c, (unsigned long long)__shfl_xor((long long)c, o, 64));
+      kth = max64(kth, c);
     }
-    if (n <= BF_CAP) break;
-    __syncthreads();
-    bound = s_bound[0];
-    if (tid == 0) s_n = 0;
-    __syncthreads();
-  }
-  for (int i = n + tid; i < K; i += NT) {
-    const size_t o = (size_t)grp * K + i;
-    a.scores_out[o] = -INFINITY;
-    a.beam_out[o] = -1;
-    a.token_out[o] = -1;
+    Cand bound = {kth, 0, 0x7FFFFFFF};     // entries with its score are at or before it
+    for (;;) {
+#pragma unroll
+      for (int j = 0; j < BF_PER; ++j) {
+        if (e0 + j * BF_THREADS < entries) {
+          const bool in = so[j] != 0 && !before(bound, {so[j], key[j], beam[j]});
+          const unsigned long long who = __ballot(in);
+          if (who) {
+            int at = 0;                    // where an entry lies does not matter: they are ranked below
+            if (lane == 0) at = atomicAdd(&s_n, __popcll(who));
+            at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & ((1ull << lane) - 1));
+            if (in && at < BF_CAP) {
+              s_so[at] = so[j];
+              s_key[at] = key[j];
+              s_beam[at] = beam[j];
+            }
+          }
+        }
+      }
+      __syncthreads();
+      const int n = s_n, have = min(n, BF_CAP);
+      const bool over = n > BF_CAP, last = e0 + BF_THREADS * BF_PER >= entries;
+      // G threads count what goes before an entry
+      int G = 1;
+      while (G < 64 && 2 * G * have <= BF_THREADS) G *= 2;
+      for (int i0 = 0; i0 < have; i0 += BF_THREADS / G) {
+        const int i = i0 + tid / G;
+        const int ic = min(i, have - 1);
+        const Cand c = {s_so[ic], s_key[ic], s_beam[ic]};
+        int above = 0;
+#pragma unroll 2
+        for (int o = tid % G; o < have; o += G) above += before({s_so[o], s_key[o], s_beam[o]}, c);
+        for (int o = 1; o < G; o <<= 1) above += __shfl_xor(above, o, 64);
+        if (i < have && above < K && tid % G == 0) {
+          if (last && !over) {
+            const size_t o = (size_t)grp * K + above;
+            a.scores_out[o] = (float)unord64(c.score);
+            a.beam_out[o] = c.beam;
+            a.token_out[o] = (int32_t)(0xFFFFFFFFu - (unsigned)c.key);
+          } else {
+            s_keep_so[above] = c.score;
+            s_keep_key[above] = c.key;
+            s_keep_beam[above] = c.beam;
+          }
+        }
+      }
+      if (!over && last) {
+        for (int i = have + tid; i < K; i += BF_THREADS) {
+          const size_t o = (size_t)grp * K + i;
+          a.scores_out[o] = -INFINITY;
+          a.beam_out[o] = -1;
+          a.token_out[o] = -1;
+        }
+        return;
+      }
+      __syncthreads();
+      if (over) {                          // more than there is room for (many equal scores): the K-th of those at hand bounds more tightly
+        bound = {s_keep_so[K - 1], s_keep_key[K - 1], s_keep_beam[K - 1]};
+      } else {
+        kept = min(have, K);
+        for (int i = tid; i < kept; i += BF_THREADS) {
+          s_so[i] = s_keep_so[i];
+          s_key[i] = s_keep_key[i];
+          s_beam[i] = s_keep_beam[i];
+        }
+        if (kept == K) kth = max64(kth, s_keep_so[K - 1]);
+      }
+      if (tid == 0) s_n = kept;
+      __syncthreads();
+      if (!over) break;
+    }
   }
 }
 
 BeamScratch beam_scratch(int rows, int vocab, int n_keep, void *base, size_t *bytes) {
+  // A round of 2048 logits per wavefront, as long as that makes no more wavefronts than the chip holds four to a SIMD: every
+  // stretch costs a threshold, a ranking and a list.
   BeamScratch w;
-  w.pieces = (vocab + BS_PIECE - 1) / BS_PIECE;
+  const int rounds = (vocab + 64 * BS_PER - 1) / (64 * BS_PER), most = std::max(1, 4096 / rows);
+  w.rounds = (rounds + most - 1) / most;
+  w.pieces = (rounds + w.rounds - 1) / w.rounds;
   const size_t lists = (size_t)rows * w.pieces, ms = align_up(lists * sizeof(float2), 256);
   w.ms = (float2 *)base;
   w.keys = (unsigned long long *)((char *)base + ms);
@@ -412,13 +510,15 @@ size_t beam_select_bytes(int n_groups, int n_beams, int vocab, int n_keep) {
 
 hipError_t launch_beam_select(const BeamSelect &a, void *scratch, hipStream_t s) {
   size_t bytes;
-  const BeamScratch w = beam_scratch(a.n_groups * a.n_beams, a.vocab, a.n_keep, scratch, &bytes);
+  BeamScratch w = beam_scratch(a.n_groups * a.n_beams, a.vocab, a.n_keep, scratch, &bytes);
+  w.by_lists = FastDiv(a.n_beams * w.pieces);
+  w.by_beams = FastDiv(a.n_beams);
   const dim3 grid(w.pieces, a.n_groups * a.n_beams);
   if (a.logits_dtype == 0) hipLaunchKernelGGL(beam_stretch_kernel<float>, grid, dim3(64), 0, s, a, w);
   else hipLaunchKernelGGL(beam_stretch_kernel<bf16>, grid, dim3(64), 0, s, a, w);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(beam_final_kernel, dim3(a.n_groups), dim3(64 * BF_WAVES), 0, s, a, w);
+  hipLaunchKernelGGL(beam_final_kernel, dim3(a.n_groups), dim3(BF_THREADS), 0, s, a, w);
   return hipGetLastError();
 }
 

@@ -6,6 +6,16 @@
 
 namespace cb {
 
+// n / d by a multiplication: m = 2^32 / d rounded down (d = 1: 2^32 - 1) gives a quotient at most one too small for n < 2^31
+struct FastDiv {
+  unsigned d, m;
+  FastDiv(unsigned div = 1) : d(div), m(div == 1 ? 0xFFFFFFFFu : (unsigned)((1ull << 32) / div)) {}
+  __host__ __device__ unsigned div(unsigned n) const {
+    const unsigned q = (unsigned)(((unsigned long long)n * m) >> 32);
+    return q + (n - q * d >= d);
+  }
+};
+
 // Device table of the requests stacked in one layer call, kSegInts ints per request (+ one closing
 // entry whose kSegQwg is the total): where its rows enter (kSegInOff) and how many of them are
 // candidates / kept / suffix rows, where its kept rows start in the output (kSegOutOff), its first
@@ -169,15 +179,6 @@ hipError_t launch_lm_head(int dtype, const float *h_row, const void *gain, const
 // Attention of n_groups x n_seqs continuations, n_q query rows each, over their group's context and their own tail:
 // row r (of continuation r / n_q) sees ctx_len[group] rows of its group's slab of kc / vc and the first row_tail[r] rows of its
 // continuation's slab of kt / vt; row_tail[r] < 0 marks a padding row, whose output is zero.
-// n / d by a multiplication: m = 2^32 / d rounded down (d = 1: 2^32 - 1) gives a quotient at most one too small for n < 2^31
-struct FastDiv {
-  unsigned d, m;
-  FastDiv(unsigned div = 1) : d(div), m(div == 1 ? 0xFFFFFFFFu : (unsigned)((1ull << 32) / div)) {}
-  __host__ __device__ unsigned div(unsigned n) const {
-    const unsigned q = (unsigned)(((unsigned long long)n * m) >> 32);
-    return q + (n - q * d >= d);
-  }
-};
 constexpr int kSharedGroups = 64;          // groups per launch (their context lengths travel as arguments)
 struct SharedAttn {
   const void *q, *kc, *vc, *kt, *vt;       // q, o: [rows, Hq, dh]; caches [*, Hkv, dh]
