@@ -18,5 +18,6 @@ _BINDING_NAMES = ("Context", "CacheBlendError", "cb_create", "cb_destroy", "cb_s
 def __getattr__(name):
     if name in _BINDING_NAMES:
         from . import binding
-        return getattr(binding, name)
+        value = globals()[name] = getattr(binding, name)       # found without this function from now on
+        return value
     raise AttributeError(name)

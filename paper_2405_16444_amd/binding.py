@@ -439,11 +439,22 @@ def cb_first_token(ctx: Context, final_hidden: torch.Tensor, final_norm: torch.T
     return logits, token
 
 
-def _caches(ctx: Context, k: torch.Tensor, v: torch.Tensor):
-    """Checks a K and a V array [rows, Hkv, dh] of the context's type."""
-    m = ctx.model
-    assert k.dtype == ctx.dtype and v.dtype == ctx.dtype and k.is_contiguous() and v.is_contiguous()
-    assert k.shape == v.shape and k.shape[1:] == (m.n_kv_heads, m.head_dim) and k.device == ctx.device and v.device == ctx.device
+# The calls below run once per layer and token, in a few microseconds: their checks are kept to what a tensor costs least to tell.
+def _current_stream(ctx: Context, stream) -> int:
+    """Handle of `stream`, None: of the current stream of the context's device."""
+    return torch._C._cuda_getCurrentRawStream(ctx.device.index) if stream is None else stream.cuda_stream
+
+
+def _fits(ctx: Context, t: torch.Tensor, dtype, shape) -> bool:
+    """A contiguous tensor of that type and shape on the context's device"""
+    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == ctx.device.index
+
+
+def _cache_rows(ctx: Context, k: torch.Tensor, v: torch.Tensor) -> int:
+    """Rows of a K and a V array [rows, Hkv, dh], checked"""
+    shape = (k.shape[0], ctx.model.n_kv_heads, ctx.model.head_dim)
+    assert _fits(ctx, k, ctx.dtype, shape) and _fits(ctx, v, ctx.dtype, shape)
+    return shape[0]
 
 
 def cb_qkv_norm_rope(ctx: Context, qkv, row_pos: torch.Tensor, cache_row: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -451,31 +462,33 @@ def cb_qkv_norm_rope(ctx: Context, qkv, row_pos: torch.Tensor, cache_row: torch.
                      q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Normalised, rotated queries [n_rows, Hq, dh] (returned); keys and values go into rows cache_row of the caches.
     qkv: one projection output [n_rows, (Hq + 2 Hkv) dh], or the three as (q, k, v); rows may be strided."""
-    m, dev = ctx.model, ctx.device
-    dh, nq, nk = m.head_dim, m.n_q_heads * m.head_dim, m.n_kv_heads * m.head_dim
+    m, dt, dev = ctx.model, ctx.dtype, ctx.device.index
+    hq, dh = m.n_q_heads, m.head_dim
+    nq, nk = hq * dh, m.n_kv_heads * dh
     if isinstance(qkv, torch.Tensor):
-        n_rows, width = qkv.shape
-        assert qkv.dtype == ctx.dtype and qkv.device == dev and width == nq + 2 * nk and (qkv.stride(1) == 1 or n_rows == 0)
-        qs = ks = vs = qkv.stride(0) if n_rows > 1 else width
-        es, q = qkv.element_size(), qkv.data_ptr()
+        (n_rows, width), (qs, inner) = qkv.shape, qkv.stride()
+        assert qkv.dtype is dt and qkv.get_device() == dev and width == nq + 2 * nk and (inner == 1 or n_rows == 0)
+        qs = ks = vs = qs if n_rows > 1 else width
+        q, es = qkv.data_ptr(), qkv.element_size()
         k, v = q + nq * es, q + (nq + nk) * es
     else:
         n_rows = qkv[0].shape[0]
         for t, w in zip(qkv, (nq, nk, nk)):
-            assert t.dtype == ctx.dtype and t.device == dev and t.shape == (n_rows, w) and (t.stride(1) == 1 or n_rows == 0)
+            assert t.dtype is dt and t.get_device() == dev and t.shape == (n_rows, w) and (t.stride(1) == 1 or n_rows == 0)
         q, k, v = (t.data_ptr() for t in qkv)
         qs, ks, vs = (t.stride(0) if n_rows > 1 else w for t, w in zip(qkv, (nq, nk, nk)))
-    for t in (row_pos, cache_row):
-        assert t.dtype == torch.int32 and t.shape == (n_rows,) and t.is_contiguous() and t.device == dev
-    for t in (q_norm, k_norm):
-        assert t is None or (t.dtype == ctx.dtype and t.shape == (dh,) and t.is_contiguous() and t.device == dev)
-    _caches(ctx, k_cache, v_cache)
+    assert _fits(ctx, row_pos, torch.int32, (n_rows,)) and _fits(ctx, cache_row, torch.int32, (n_rows,))
+    assert q_norm is None or _fits(ctx, q_norm, dt, (dh,))
+    assert k_norm is None or _fits(ctx, k_norm, dt, (dh,))
+    cache_rows = _cache_rows(ctx, k_cache, v_cache)
     if q_out is None:
-        q_out = torch.empty((n_rows, m.n_q_heads, dh), dtype=ctx.dtype, device=dev)
-    assert q_out.dtype == ctx.dtype and q_out.device == dev and q_out.is_contiguous() and q_out.shape == (n_rows, m.n_q_heads, dh)
-    _check(_lib.cb_qkv_norm_rope(ctx._h, q, qs, k, ks, v, vs, _ptr(q_norm), _ptr(k_norm), row_pos.data_ptr(), cache_row.data_ptr(),
-                                 n_rows, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_cache.shape[0], _stream(stream)),
-           "cb_qkv_norm_rope")
+        q_out = torch.empty((n_rows, hq, dh), dtype=dt, device=ctx.device)
+    else:
+        assert _fits(ctx, q_out, dt, (n_rows, hq, dh))
+    status = _lib.cb_qkv_norm_rope(ctx._h, q, qs, k, ks, v, vs, None if q_norm is None else q_norm.data_ptr(),
+                                   None if k_norm is None else k_norm.data_ptr(), row_pos.data_ptr(), cache_row.data_ptr(), n_rows,
+                                   q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache_rows, _current_stream(ctx, stream))
+    _check(status, "cb_qkv_norm_rope")
     return q_out
 
 
@@ -489,26 +502,26 @@ def cb_shared_prefix_attention(ctx: Context, q: torch.Tensor, n_groups: int, n_s
                                stream=None) -> torch.Tensor:
     """Attention of n_groups x n_seqs continuations over their group's context and their own tails.  q [rows, Hq, dh]; k_prefix / v_prefix
     [n_groups * prefix_stride, Hkv, dh]; k_tail / v_tail [n_groups * n_seqs * tail_stride, Hkv, dh]; row_tail int32 [rows]."""
-    m, dev = ctx.model, ctx.device
-    seqs = n_groups * n_seqs
+    m, seqs = ctx.model, n_groups * n_seqs
     rows = seqs * n_q
+    shape = (rows, m.n_q_heads, m.head_dim)
     assert n_groups >= 1 and n_seqs >= 1 and n_q >= 1 and len(prefix_lens) == n_groups
-    assert q.dtype == ctx.dtype and q.device == dev and q.is_contiguous() and q.shape == (rows, m.n_q_heads, m.head_dim)
-    assert row_tail.dtype == torch.int32 and row_tail.shape == (rows,) and row_tail.is_contiguous() and row_tail.device == dev
-    _caches(ctx, k_prefix, v_prefix)
-    _caches(ctx, k_tail, v_tail)
-    assert k_prefix.shape[0] % n_groups == 0 and k_tail.shape[0] % seqs == 0
-    prefix_stride, tail_stride = k_prefix.shape[0] // n_groups, k_tail.shape[0] // seqs
+    assert _fits(ctx, q, ctx.dtype, shape) and _fits(ctx, row_tail, torch.int32, (rows,))
+    prefix_stride, rest = divmod(_cache_rows(ctx, k_prefix, v_prefix), n_groups)
+    tail_stride, rest_tail = divmod(_cache_rows(ctx, k_tail, v_tail), seqs)
+    assert rest == 0 and rest_tail == 0
     if out is None:
         out = torch.empty_like(q)
-    assert out.dtype == ctx.dtype and out.device == dev and out.is_contiguous() and out.shape == q.shape
+    else:
+        assert _fits(ctx, out, ctx.dtype, shape)
     if workspace is None:
         workspace = torch.empty(cb_shared_prefix_workspace_bytes(ctx, n_groups, n_seqs, n_q, max(prefix_lens), tail_stride),
-                                dtype=torch.uint8, device=dev)
-    _check(_lib.cb_shared_prefix_attention(ctx._h, q.data_ptr(), n_groups, n_seqs, n_q, k_prefix.data_ptr(), v_prefix.data_ptr(),
-                                           (C.c_int32 * n_groups)(*prefix_lens), prefix_stride, k_tail.data_ptr(), v_tail.data_ptr(),
-                                           tail_stride, row_tail.data_ptr(), out.data_ptr(), workspace.data_ptr(),
-                                           workspace.numel(), _stream(stream)), "cb_shared_prefix_attention")
+                                dtype=torch.uint8, device=ctx.device)
+    status = _lib.cb_shared_prefix_attention(ctx._h, q.data_ptr(), n_groups, n_seqs, n_q, k_prefix.data_ptr(), v_prefix.data_ptr(),
+                                             (C.c_int32 * n_groups)(*prefix_lens), prefix_stride, k_tail.data_ptr(), v_tail.data_ptr(),
+                                             tail_stride, row_tail.data_ptr(), out.data_ptr(), workspace.data_ptr(),
+                                             workspace.numel(), _current_stream(ctx, stream))
+    _check(status, "cb_shared_prefix_attention")
     return out
 
 
@@ -521,27 +534,27 @@ def cb_beam_select(ctx: Context, logits: torch.Tensor, scores: torch.Tensor, n_g
                    out=None):
     """(scores float, beam int32, token int32), each [n_groups, n_keep], best first.  logits [n_groups * n_beams, vocab] float or bfloat16,
     rows may be strided; scores float [n_groups * n_beams]; finished None or int32 of the same size.  out: the three results' tensors."""
-    dev = ctx.device
-    rows, vocab = logits.shape
-    assert n_groups >= 1 and rows >= n_groups and rows % n_groups == 0 and logits.device == dev
-    assert logits.dtype in (torch.float32, torch.bfloat16) and (logits.stride(1) == 1 or vocab == 1)
-    assert scores.dtype == torch.float32 and scores.numel() == rows and scores.is_contiguous() and scores.device == dev
-    if finished is not None:
-        assert finished.dtype == torch.int32 and finished.numel() == rows and finished.is_contiguous() and finished.device == dev
+    (rows, vocab), (stride, inner) = logits.shape, logits.stride()
+    half = logits.dtype is torch.bfloat16
+    assert n_groups >= 1 and rows >= n_groups and rows % n_groups == 0 and logits.get_device() == ctx.device.index
+    assert (half or logits.dtype is torch.float32) and (inner == 1 or vocab == 1)
+    assert _fits(ctx, scores, torch.float32, (rows,)) and (finished is None or _fits(ctx, finished, torch.int32, (rows,)))
+    shape = (n_groups, n_keep)
     if out is None:
-        out = (torch.empty((n_groups, n_keep), dtype=torch.float32, device=dev),
-               torch.empty((n_groups, n_keep), dtype=torch.int32, device=dev),
-               torch.empty((n_groups, n_keep), dtype=torch.int32, device=dev))
-    for t, dt in zip(out, (torch.float32, torch.int32, torch.int32)):
-        assert t.dtype == dt and t.numel() == n_groups * n_keep and t.is_contiguous() and t.device == dev
+        # beams and tokens lie side by side: one allocation
+        ints = torch.empty((2, n_groups, n_keep), dtype=torch.int32, device=ctx.device)
+        out = (torch.empty(shape, dtype=torch.float32, device=ctx.device), ints[0], ints[1])
+    else:
+        assert _fits(ctx, out[0], torch.float32, shape) and _fits(ctx, out[1], torch.int32, shape) and _fits(ctx, out[2], torch.int32, shape)
     n_beams = rows // n_groups
     if workspace is None:
         workspace = torch.empty(max(256, cb_beam_select_workspace_bytes(ctx, n_groups, n_beams, vocab, n_keep)), dtype=torch.uint8,
-                                device=dev)
-    _check(_lib.cb_beam_select(ctx._h, logits.data_ptr(), CB_F32 if logits.dtype == torch.float32 else CB_BF16,
-                               logits.stride(0) if rows > 1 else vocab, n_groups, n_beams, vocab, scores.data_ptr(), _ptr(finished),
-                               end_token, n_keep, out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), workspace.data_ptr(),
-                               workspace.numel(), _stream(stream)), "cb_beam_select")
+                                device=ctx.device)
+    status = _lib.cb_beam_select(ctx._h, logits.data_ptr(), CB_BF16 if half else CB_F32, stride if rows > 1 else vocab, n_groups, n_beams,
+                                 vocab, scores.data_ptr(), None if finished is None else finished.data_ptr(), end_token, n_keep,
+                                 out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                 _current_stream(ctx, stream))
+    _check(status, "cb_beam_select")
     return out
 
 
@@ -549,15 +562,14 @@ def _layer_ptrs(ctx: Context, layers):
     """Pointers of per-layer arrays [rows, Hkv, dh]: a sequence of tensors, or one tensor with the layers in front; and their rows."""
     m = ctx.model
     if isinstance(layers, torch.Tensor):
-        assert layers.dtype == ctx.dtype and layers.is_contiguous() and layers.device == ctx.device
-        assert layers.dim() == 4 and layers.shape[2:] == (m.n_kv_heads, m.head_dim)
-        n, base, step = layers.shape[0], layers.data_ptr(), layers.stride(0) * layers.element_size()
-        return (C.c_void_p * n)(*[base + i * step for i in range(n)]), n, layers.shape[1]
+        n, rows = layers.shape[:2]
+        assert _fits(ctx, layers, ctx.dtype, (n, rows, m.n_kv_heads, m.head_dim))
+        base, step = layers.data_ptr(), layers.stride(0) * layers.element_size()
+        return (C.c_void_p * n)(*range(base, base + n * step, step)) if n * step else (C.c_void_p * n)(), n, rows
     rows = layers[0].shape[0]
     for t in layers:
-        assert t.dtype == ctx.dtype and t.is_contiguous() and t.device == ctx.device
-        assert t.shape == (rows, m.n_kv_heads, m.head_dim)
-    return _ptr_array(layers), len(layers), rows
+        assert _fits(ctx, t, ctx.dtype, (rows, m.n_kv_heads, m.head_dim))
+    return (C.c_void_p * len(layers))(*[t.data_ptr() for t in layers]), len(layers), rows
 
 
 def cb_beam_reorder(ctx: Context, k_tail_layers, v_tail_layers, n_groups: int, parent: torch.Tensor,
@@ -568,10 +580,10 @@ def cb_beam_reorder(ctx: Context, k_tail_layers, v_tail_layers, n_groups: int, p
     v, nv, rows_v = _layer_ptrs(ctx, v_tail_layers)
     beams = parent.numel()
     assert nk == nv and rows == rows_v and n_groups >= 1 and beams >= n_groups and beams % n_groups == 0 and rows % beams == 0
-    for t in (parent, seq_len):
-        assert t is None or (t.dtype == torch.int32 and t.numel() == beams and t.is_contiguous() and t.device == ctx.device)
-    _check(_lib.cb_beam_reorder(ctx._h, k, v, 0, nk, n_groups, beams // n_groups, rows // beams, parent.data_ptr(), _ptr(seq_len),
-                                _stream(stream)), "cb_beam_reorder")
+    assert _fits(ctx, parent, torch.int32, (beams,)) and (seq_len is None or _fits(ctx, seq_len, torch.int32, (beams,)))
+    status = _lib.cb_beam_reorder(ctx._h, k, v, 0, nk, n_groups, beams // n_groups, rows // beams, parent.data_ptr(),
+                                  None if seq_len is None else seq_len.data_ptr(), _current_stream(ctx, stream))
+    _check(status, "cb_beam_reorder")
 
 
 def cb_recompute_delay(ratio: float, prefill_delay: float) -> float:

@@ -113,11 +113,10 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// One wavefront: a stretch of a row, 64 x BS_PER logits at a time, the next ones on their way meanwhile.  Bound by HBM where there are many
-// rows, so the instructions per logit count: the running maximum and sum of exponentials, kept per lane and joined at the end
+// One wavefront: a stretch of a row, 64 x BS_PER logits at a time (the next ones on their way meanwhile would take the registers of the wavefronts
+// that hide the loads).  Bound by HBM where there are many rows, so the instructions per logit count: the running maximum and sum of exponentials, kept per lane and joined at the end
 // (a subtraction, a product, an exponential, an addition), and one comparison with the threshold.  The threshold comes from the first
-// round: what can be among the n_keep best lies in the n_keep lanes with the largest maxima, at or above the
-// n_keep-th largest of them.  What passes it goes to a list that is ranked at the end, or when it is half full, which
+// round: n_keep lanes have maxima at or above the n_keep-th largest of the lanes' maxima, so nothing below it is wanted.  What passes it goes to a list that is ranked at the end, or when it is half full, which
 // tightens the threshold; where it overflows (many equal logits), the n_keep-th of those at hand does, and the round is gone through again.
 template <typename TL>
 __global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScratch w) {
@@ -125,35 +124,41 @@ __global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScra
   constexpr int N = V::N, NV = BS_PER / N;
   constexpr float kLog2e = 1.4426950408889634f;
   __shared__ unsigned long long s_list[BS_CAP];
+  __shared__ __attribute__((aligned(16))) float s_x[64 * BS_PER];
   const int row = blockIdx.y, piece = blockIdx.x, lane = threadIdx.x, K = a.n_keep;
   if (a.finished && a.finished[row] != 0) return;
   const TL *src = (const TL *)a.logits + (size_t)row * a.row_stride;
   // Which lane adds up which tokens depends on the tokens alone, so that equal rows have equal sums wherever they start: 16-byte loads at any
-  // alignment of the type (the hardware takes them), the last vector of a row element by element.
+  // alignment of the type (the hardware takes them), a row's last round element by element.
   const int t0 = piece * w.rounds * (64 * BS_PER) + lane * N;
+  const int n_rounds = min(w.rounds, (a.vocab + 64 * BS_PER - 1) / (64 * BS_PER) - piece * w.rounds);
   V raw[NV];
   auto load = [&](int round) {
+    const char *base = (const char *)src + (size_t)(piece * w.rounds + round) * (64 * BS_PER) * sizeof(TL);
+    const int left = a.vocab - (piece * w.rounds + round) * (64 * BS_PER);
+    if (left >= 64 * BS_PER) {             // the same for all lanes: no branch between the loads
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int t = t0 + (round * NV + i) * 64 * N;
-      if (t + N <= a.vocab) {
-        __builtin_memcpy(&raw[i], src + t, sizeof(V));
-      } else {
+      for (int i = 0; i < NV; ++i) __builtin_memcpy(&raw[i], base + (unsigned)((i * 64 + lane) * sizeof(V)), sizeof(V));
+    } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) raw[i].set(j, t + j < a.vocab ? to_f32(src[t + j]) : -INFINITY);
-      }
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const int t = (i * 64 + lane) * N + j;
+          const float v = to_f32(*(const TL *)(base + (unsigned)(min(t, left - 1) * (int)sizeof(TL))));
+          raw[i].set(j, t < left ? v : -INFINITY);
+        }
     }
   };
-  load(0);
   float lm = -INFINITY, ls = 0.f, tv = -INFINITY;
   unsigned long long thr = 0;
   int n = 0;
 #pragma unroll 1
-  for (int round = 0; round < w.rounds; ++round) {
+  for (int round = 0; round < n_rounds; ++round) {
+    load(round);
     float x[BS_PER];
 #pragma unroll
     for (int i = 0; i < BS_PER; ++i) x[i] = fmaxf(raw[i / N].get(i % N), -INFINITY);      // NaN counts as -infinity
-    if (round + 1 < w.rounds) load(round + 1);
     const int tr = t0 + round * 64 * BS_PER;
     auto token = [&](int i) { return tr + i / N * 64 * N + i % N; };
     float m = -INFINITY;
@@ -175,34 +180,34 @@ __global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScra
     }
     lm = nm;
     if (round == 0) {
-      unsigned long long best = 0;         // the lane's best key: the lowest of its tokens with the maximum
-#pragma unroll
-      for (int i = BS_PER - 1; i >= 0; --i)
-        if (x[i] == m) best = logit_key(m, token(i));
-      int rank = 0;
-#pragma unroll 8
-      for (int l = 0; l < 64; ++l) rank += lane_value(best, l) > best;
-      const unsigned long long kth = __ballot(rank == K - 1 && best != 0);
-      if (kth) {
-        thr = lane_value(best, __ffsll((long long)kth) - 1);
-        tv = unord32((unsigned)(thr >> 32));
-      }
+      int at_least = 0;                    // lanes whose maximum is no smaller
+#pragma unroll 16
+      for (int l = 0; l < 64; ++l) at_least += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(m), l)) >= m;
+      tv = wave_max(at_least >= K ? m : -INFINITY);
     }
     const int kept = n;
-    const bool last = round + 1 == w.rounds;
+    const bool last = round + 1 == n_rounds;
     bool over = __any(m >= tv) || last;
+    // The logits at or above the threshold, one per lane at a time: which of its registers a lane takes differs, so they are read back
+    // from LDS.  (Register by register, each behind a branch, this took 23000 clocks instead of 2000, mostly to fetch the code.)
+    if (over) {
+#pragma unroll
+      for (int i = 0; i < BS_PER; i += 4) *reinterpret_cast<f32x4 *>(&s_x[i * 64 + lane * 4]) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+    }
     while (over) {
       n = kept;
+      unsigned todo = 0;
 #pragma unroll
-      for (int i = 0; i < BS_PER; ++i) {
-        if (__any(x[i] >= tv)) {
-          const unsigned long long key = logit_key(x[i], token(i));
-          const bool in = key != 0 && key >= thr;
-          const unsigned long long who = __ballot(in);
-          const int at = n + __popcll(who & ((1ull << lane) - 1));
-          if (in && at < BS_CAP) s_list[at] = key;
-          n += __popcll(who);
-        }
+      for (int i = 0; i < BS_PER; ++i) todo |= x[i] >= tv ? 1u << i : 0u;
+      while (__any(todo != 0)) {
+        const int i = todo ? __ffs((int)todo) - 1 : 0;
+        const unsigned long long key = logit_key(s_x[(i & ~3) * 64 + lane * 4 + (i & 3)], token(i));
+        const bool in = todo != 0 && key != 0 && key >= thr;
+        const unsigned long long who = __ballot(in);
+        const int at = n + __popcll(who & ((1ull << lane) - 1));
+        if (in && at < BS_CAP) s_list[at] = key;
+        n += __popcll(who);
+        todo &= todo - 1;
       }
       over = n > BS_CAP;
       if (!over && !last && n <= BS_CAP / 2) break;
