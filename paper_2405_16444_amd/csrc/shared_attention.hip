@@ -108,11 +108,13 @@ __device__ __forceinline__ void store_empty(const SharedAttn &a, const Item &it,
 // tiles' results are joined in LDS.
 // ---------------------------------------------------------------------------
 constexpr int shared_ring_bytes(int dh, int ks, int st) { return ks * st * 2 * SA_TILE * dh * 2; }
-template <int DH, int QB, int KS, int ST>
-__global__ __launch_bounds__(64 * QB * KS) void shared_attn_bf16_kernel(SharedAttn a) {
+// RAGGED: several new tokens per continuation (n_q > 1), which see different tail rows and may be padding.  Else everything in the item's range
+// is seen by all of its queries.
+template <int DH, int QB, int KS, int ST, bool RAGGED>
+__global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16_kernel(SharedAttn a) {
   constexpr int ROWB = DH * 2, CH = DH / 8, RPI = 1024 / ROWB, TB = SA_TILE * ROWB, LPT = SA_TILE / RPI, LPW = 2 * LPT / QB;
   constexpr int NKS = DH / 32, NCB = DH / 16, NQ = 16 * QB;
-  static_assert(LPW >= 1 && ST >= 2 && ST <= 4 && NCB % KS == 0, "loads, waits and channels are shared out evenly");
+  static_assert(LPW >= 1 && ST >= 1 && ST <= 4 && NCB % KS == 0, "loads, waits and channels are shared out evenly");
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, h = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qb = wave % QB, ks = wave / QB;
@@ -124,9 +126,8 @@ __global__ __launch_bounds__(64 * QB * KS) void shared_attn_bf16_kernel(SharedAt
   // A context is seen whole by every query; which tail rows are, and whether a block is all padding, has to be read.
   const int m = it.m0 + qb * 16 + ln, mc = min(m, it.m_end - 1), r = (int)a.by_g.div(mc);
   int vis = it.limit, kv_len = it.limit, min_vis = it.limit;
-  if (it.tail && a.n_q == 1) {
-    vis = kv_len = min_vis = min(max(a.row_tail[it.row0], 0), it.limit);
-  } else if (a.n_q > 1) {
+  if (!RAGGED && it.tail) kv_len = min_vis = min(max(a.row_tail[it.row0], 0), it.limit);
+  if (RAGGED) {
     bool real;
     vis = visible(a, it, m, &real);
     kv_len = 0;
@@ -162,19 +163,21 @@ __global__ __launch_bounds__(64 * QB * KS) void shared_attn_bf16_kernel(SharedAt
   auto issue = [&](int t, int stage) {
     const int last = kv_len - 1 - t * SA_TILE;            // rows past the end repeat the last one
     const size_t tile0 = (size_t)t * (SA_TILE * (size_t)row_bytes);
+    unsigned lr = lrow, kc = kcol, vc = vcol;             // what follows is computed here, not kept in registers across the loop
+    asm volatile("" : "+v"(lr), "+v"(kc), "+v"(vc));
 #pragma unroll
     for (int j = 0; j < LPW; ++j) {
       const int l = qb * LPW + j, i = l & (LPT - 1);
       const bool is_v = l >= LPT;
-      const unsigned col = is_v ? vcol ^ (fv(i * RPI) * 16) : kcol ^ (fk(i * RPI) * 16);
-      const char *src = (is_v ? it.v : it.k) + tile0 + (unsigned)(min((int)(i * RPI + lrow), last) * row_bytes + col);
+      const unsigned col = is_v ? vc ^ (fv(i * RPI) * 16) : kc ^ (fk(i * RPI) * 16);
+      const char *src = (is_v ? it.v : it.k) + tile0 + (unsigned)(min((int)(i * RPI + lr), last) * row_bytes + col);
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
                                        (__attribute__((address_space(3))) void *)(ring + stage * 2 * TB + l * 1024), 16, 0, 0);
     }
   };
   const int n_it = (t_end - t_begin + KS - 1) / KS, n_mine = (t_end - t_begin - ks + KS - 1) / KS;
 #pragma unroll
-  for (int i = 0; i < ST - 1; ++i)
+  for (int i = 0; i < (ST > 1 ? ST - 1 : 1); ++i)
     if (i < n_mine) issue(t_begin + i * KS + ks, i);
 
   bf16x8 qf[NKS];
@@ -205,40 +208,37 @@ __global__ __launch_bounds__(64 * QB * KS) void shared_attn_bf16_kernel(SharedAt
     else vm_wait<0>();
     if (QB > 1) asm volatile("s_barrier" ::: "memory");
     // the stage of tile i - 1, which everybody has read, takes tile i + ST - 1
-    if (i + ST - 1 < n_mine) issue(t_begin + (i + ST - 1) * KS + ks, stage == 0 ? ST - 1 : stage - 1);
-    if (i >= n_mine) continue;
+    if (ST > 1 && i + ST - 1 < n_mine) issue(t_begin + (i + ST - 1) * KS + ks, stage == 0 ? ST - 1 : stage - 1);
+    if (i >= n_mine) continue;           // (with one stage: only in the last iteration)
     const int t0 = (t_begin + i * KS + ks) * SA_TILE;
     const unsigned so = stage * 2 * TB;
-    bf16x8 kf[2][NKS];
-    if constexpr (NKS == 4) {
-      asm volatile(
-          "ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\tds_read_b128 %3, %11\n\t"
-          "ds_read_b128 %4, %8 offset:4096\n\tds_read_b128 %5, %9 offset:4096\n\t"
-          "ds_read_b128 %6, %10 offset:4096\n\tds_read_b128 %7, %11 offset:4096\n\ts_waitcnt lgkmcnt(0)"
-          : "=&v"(kf[0][0]), "=&v"(kf[0][1]), "=&v"(kf[0][2]), "=&v"(kf[0][3]), "=&v"(kf[1][0]), "=&v"(kf[1][1]),
-            "=&v"(kf[1][2]), "=&v"(kf[1][3])
-          : "v"(ka0 + so), "v"((ka0 + so) ^ 64), "v"((ka0 + so) ^ 128), "v"((ka0 + so) ^ 192)
-          : "memory");
-    } else {
-      asm volatile(
-          "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %4 offset:2048\n\t"
-          "ds_read_b128 %3, %5 offset:2048\n\ts_waitcnt lgkmcnt(0)"
-          : "=&v"(kf[0][0]), "=&v"(kf[0][1]), "=&v"(kf[1][0]), "=&v"(kf[1][1])
-          : "v"(ka0 + so), "v"((ka0 + so) ^ 64)
-          : "memory");
-    }
     const bool masked = t0 + SA_TILE > min_vis;           // some key of the tile is hidden from some query
     f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int k = 0; k < NKS; ++k)
+    for (int kb = 0; kb < 2; ++kb) {                       // 16 keys at a time: with all 32 the registers of two workgroups would not fit
+      bf16x8 kf[NKS];
+      if constexpr (NKS == 4)
+        asm volatile(
+            "ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%8\n\tds_read_b128 %2, %6 offset:%8\n\t"
+            "ds_read_b128 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(kf[0]), "=&v"(kf[1]), "=&v"(kf[2]), "=&v"(kf[3])
+            : "v"(ka0 + so), "v"((ka0 + so) ^ 64), "v"((ka0 + so) ^ 128), "v"((ka0 + so) ^ 192), "n"(kb * 16 * ROWB)
+            : "memory");
+      else
+        asm volatile("ds_read_b128 %0, %2 offset:%4\n\tds_read_b128 %1, %3 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(kf[0]), "=&v"(kf[1])
+                     : "v"(ka0 + so), "v"((ka0 + so) ^ 64), "n"(kb * 16 * ROWB)
+                     : "memory");
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) sc[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][k], qf[k], sc[kb], 0, 0, 0);
+      for (int k = 0; k < NKS; ++k) sc[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k], qf[k], sc[kb], 0, 0, 0);
+    }
     if (masked) {
+      const int seen = RAGGED ? vis : kv_len;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (t0 + 16 * kb + 4 * h + e >= vis) sc[kb][e] = -INFINITY;
+          if (t0 + 16 * kb + 4 * h + e >= seen) sc[kb][e] = -INFINITY;
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(64 * QB * KS) void shared_attn_bf16_kernel(SharedAt
     row_sum += psum;
 #pragma unroll
     for (int c0 = 0; c0 < NCB; c0 += 4) {
-      union VF { s16x4 s[2]; bf16x8 b; } vf[4];
+      union VF { s16x4 s[2]; bf16x8 b; unsigned w[4]; } vf[4];
       asm volatile(
           "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
           "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
@@ -278,20 +278,35 @@ __global__ __launch_bounds__(64 * QB * KS) void shared_attn_bf16_kernel(SharedAt
           : "v"((va0 + so) ^ (c0 * 32)), "v"((va0 + so) ^ (c0 * 32 + 32)), "v"((va0 + so) ^ (c0 * 32 + 64)),
             "v"((va0 + so) ^ (c0 * 32 + 96)), "n"(16 * ROWB)
           : "memory");
+      // A hidden key has p = 0, but 0 times a value that is not finite is not 0.
       bool bad = false;
       if (masked) {
-        // A hidden key has p = 0, but 0 times a value that is not finite is not 0 (rows past the end repeat the last one).
+        // rows past the end repeat the last one: cleared, so that nothing is added for them
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int e = 0; e < 4; ++e) {
+          const int key = t0 + 16 * (e >> 1) + 4 * h + 2 * (e & 1);
+          const unsigned keep = key + 1 < kv_len ? 0xFFFFFFFFu : key < kv_len ? 0xFFFFu : 0u;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) bad |= !(fabsf((float)vf[c].b[e]) < INFINITY);
-        bad = __any(bad);
+          for (int c = 0; c < 4; ++c) vf[c].w[e] &= keep;
+        }
+        if (RAGGED) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {                 // two bf16 a word: an exponent of all ones is infinity or NaN
+              const unsigned word = vf[c].w[e];
+              bad |= (word & 0x7F80u) == 0x7F80u || (word & 0x7F800000u) == 0x7F800000u;
+            }
+          bad = __any(bad);
+        }
       }
-      if (__builtin_expect(!bad, 1)) {
+      if (!RAGGED || __builtin_expect(!bad, 1)) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) oacc[c0 + c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[c].b, pf, oacc[c0 + c], 0, 0, 0);
       } else {
         // the same sums key by key, over the keys that a query sees; key k of the tile is held by lane group (k % 16) / 4
+        unsigned ch = 4 * h;
+        asm volatile("" : "+v"(ch));
 #pragma unroll 1
         for (int k = 0; k < SA_TILE; ++k) {
           const int slot = (k >> 4) * 4 + (k & 3), from = ((k & 15) >> 2) * 16 + ln;
@@ -304,7 +319,7 @@ __global__ __launch_bounds__(64 * QB * KS) void shared_attn_bf16_kernel(SharedAt
           if (t0 + k < vis) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              const bf16x4 v4 = *reinterpret_cast<const bf16x4 *>(vrow + (16 * (c0 + c) + 4 * h) * 2);
+              const bf16x4 v4 = *reinterpret_cast<const bf16x4 *>(vrow + (16 * (c0 + c) + ch) * 2);
 #pragma unroll
               for (int e = 0; e < 4; ++e) oacc[c0 + c][e] = __builtin_fmaf(p, (float)v4[e], oacc[c0 + c][e]);
             }
@@ -313,6 +328,10 @@ __global__ __launch_bounds__(64 * QB * KS) void shared_attn_bf16_kernel(SharedAt
         // these loads and the ring's share a counter: with everything landed the waits that follow are met already
         vm_wait<0>();
       }
+    }
+    if (ST == 1 && i + 1 < n_it) {                        // everybody has read the tile: its place takes the next one
+      if (QB > 1) asm volatile("s_barrier" ::: "memory");
+      if (i + 1 < n_mine) issue(t_begin + (i + 1) * KS + ks, 0);
     }
   }
   row_sum = group_sum(row_sum);
@@ -600,25 +619,32 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedAttn a) {
   store4<T>((T *)a.o + ((size_t)r * a.hq + hd) * DH + c * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
-template <int DH, int QB, int KS, int ST>
+template <int DH, int QB, int KS, int ST, bool RAGGED>
 hipError_t launch_bf16(const SharedAttn &a, unsigned grid, hipStream_t s) {
   constexpr int smem = shared_ring_bytes(DH, KS, ST) + QB * KS * 16 * 8;
   static_assert(shared_ring_bytes(DH, KS, ST) >= QB * KS * (DH / 16) * 1024 || KS == 1, "the join fits in the rings' place");
   static std::once_flag once;
   std::call_once(once, [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&shared_attn_bf16_kernel<DH, QB, KS, ST>),
+    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&shared_attn_bf16_kernel<DH, QB, KS, ST, RAGGED>),
                               hipFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
-  hipLaunchKernelGGL((shared_attn_bf16_kernel<DH, QB, KS, ST>), dim3(grid), dim3(64 * QB * KS), smem, s, a);
+  hipLaunchKernelGGL((shared_attn_bf16_kernel<DH, QB, KS, ST, RAGGED>), dim3(grid), dim3(64 * QB * KS), smem, s, a);
   return hipGetLastError();
 }
 template <int DH>
 hipError_t launch_bf16_qb(const SharedAttn &a, unsigned grid, hipStream_t s) {
-  switch (a.qb) {                          // as many tiles at a time as the wavefronts leave, in at most 128 KB
-    case 1: return launch_bf16<DH, 1, 4, 2>(a, grid, s);
-    case 2: return launch_bf16<DH, 2, 4, 2>(a, grid, s);
-    case 4: return launch_bf16<DH, 4, 2, 4>(a, grid, s);
-    default: return launch_bf16<DH, 8, 1, 4>(a, grid, s);
+  // as many tiles at a time as the wavefronts leave; one new token: two workgroups to a CU, which hide each other's loads
+  if (a.n_q == 1) switch (a.qb) {
+      case 1: return launch_bf16<DH, 1, 4, 1, false>(a, grid, s);
+      case 2: return launch_bf16<DH, 2, 4, 1, false>(a, grid, s);
+      case 4: return launch_bf16<DH, 4, 2, 2, false>(a, grid, s);
+      default: return launch_bf16<DH, 8, 1, 4, false>(a, grid, s);
+    }
+  switch (a.qb) {
+    case 1: return launch_bf16<DH, 1, 4, 2, true>(a, grid, s);
+    case 2: return launch_bf16<DH, 2, 4, 2, true>(a, grid, s);
+    case 4: return launch_bf16<DH, 4, 2, 4, true>(a, grid, s);
+    default: return launch_bf16<DH, 8, 1, 4, true>(a, grid, s);
   }
 }
 
@@ -657,7 +683,7 @@ static void plan(SharedAttn &a, int max_ctx, bool may_wide, bool must_wide) {
   const int qpb = 16 * a.qb, step = SA_TILE * tiles_at_a_time(a.dtype, a.qb);
   a.ctx_blocks = (int)((ctx_q + qpb - 1) / qpb);
   a.tail_blocks = (int)((tail_q + qpb - 1) / qpb);
-  constexpr long kSlots = 256;
+  const long kSlots = a.dtype != 0 && a.n_q == 1 ? 512 : 256;
   const long ctx_units = (long)a.n_groups * a.hkv * a.ctx_blocks, tail_units = (long)a.n_groups * a.n_seqs * a.hkv * a.tail_blocks;
   a.tail_pieces = a.tail_stride == 0 ? 0 : (int)std::max<long>(1, std::min<long>((a.tail_stride + 511) / 512, kSlots / 2 / tail_units));
   if (a.wide) {
