@@ -283,8 +283,9 @@ int cb_first_token(cb_ctx *ctx, const float *final_hidden, int32_t n_suffix, con
  *               written for it
  *   cache_row : int32 [n_rows] row of the cache arrays that receives the token's K and V, outside 0 .. n_cache_rows - 1: not
  *               stored.  Two tokens with the same row leave a mixture of theirs in it
- *   q_out     : T [n_rows, n_q_heads, head_dim]; may be q itself if q_stride = n_q_heads * head_dim
- *   k_cache, v_cache : T [n_cache_rows, n_kv_heads, head_dim]; other rows are left as they were */
+ *   q_out     : T [n_rows, n_q_heads, head_dim]; may be q itself if q_stride = n_q_heads * head_dim, and overlaps no other input
+ *   k_cache, v_cache : T [n_cache_rows, n_kv_heads, head_dim]; other rows are left as they were
+ * n_rows < 2^24 (else CB_EUNSUPPORTED). */
 int cb_qkv_norm_rope(cb_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                      const void *q_norm, const void *k_norm, const int32_t *row_pos, const int32_t *cache_row, int32_t n_rows,
                      void *q_out, void *k_cache, void *v_cache, int64_t n_cache_rows, void *stream);
@@ -302,7 +303,8 @@ int cb_qkv_norm_rope(cb_ctx *ctx, const void *q, int64_t q_stride, const void *k
  * A padding row, and one that sees no key at all, gets zeros.  Hidden rows have no influence, whatever they hold (infinities and
  * NaN included).  Softmax statistics and sums are float; results do not depend on which continuations share the call but for
  * the order of additions.  prefix_stride = 0 / tail_stride = 0: no contexts / tails, their pointers are ignored.
- * The workspace bytes for max_prefix hold for every shorter context; 0: arguments out of range. */
+ * n_groups * n_seqs * n_q * n_q_heads <= 2^23 (else CB_EUNSUPPORTED).  The workspace bytes for max_prefix hold for every shorter context;
+ * 0: arguments out of range. */
 size_t cb_shared_prefix_workspace_bytes(const cb_ctx *ctx, int32_t n_groups, int32_t n_seqs, int32_t n_q, int32_t max_prefix,
                                         int32_t tail_stride);
 int cb_shared_prefix_attention(cb_ctx *ctx, const void *q, int32_t n_groups, int32_t n_seqs, int32_t n_q, const void *k_prefix,
@@ -312,11 +314,11 @@ int cb_shared_prefix_attention(cb_ctx *ctx, const void *q, int32_t n_groups, int
 
 /* The best continuations of every group: the n_keep largest of
  *     scores[beam] + logits[beam][token] - log sum_t exp(logits[beam][t])
- * over the group's beams and the vocabulary, largest first, equal ones by lower beam, then lower token; within a beam the order is
- * that of the logits.  Scores are compared in double.
+ * over the group's beams and the vocabulary, largest first, equal ones by lower beam, then larger logit, then lower token.  Scores are
+ * compared in double.
  *   logits    : logits_dtype (cb_dtype, need not be T), row r = group * n_beams + beam at logits + r * row_stride (elements); any
  *               alignment of its type.  NaN counts as -infinity; infinite logits share their beam's probability
- *   scores    : float [n_groups * n_beams], the beams' sums so far; -infinity or NaN: a beam that is not there
+ *   scores    : float [n_groups * n_beams], the beams' sums so far; one that is not finite: a beam that is not there
  *   finished  : NULL, or int32 [n_groups * n_beams]: a beam with a value other than 0 has ended; its logits are not looked at, it goes
  *               on as one continuation with its score unchanged and the token end_token (0 <= end_token < vocab)
  *   scores_out, beam_out, token_out : float, int32, int32 [n_groups * n_keep]; beam_out counts within the group.  Where a group has
@@ -357,7 +359,7 @@ int32_t cb_pick_storage_device(double recompute_delay, const double *load_delays
  * Classes: projections' main launches; attention (+ merge of key-range pieces); re-alignment; the K/V
  * projection's finish launch that also computes the deviation; selection + cache update; stand-alone
  * RMSNorm, with which a prefill call's input rows are converted and numbered; copies and other conversions; the other finish launches (sum of parked sums + residual + norm, SwiGLU
- * tail); first-token head; and two PHASES of cb_fuse_prefill / cb_fuse_prefill_pipelined that span many
+ * tail); first-token head and beam selection (cb_qkv_norm_rope counts as norm, cb_beam_reorder as copies); and two PHASES of cb_fuse_prefill / cb_fuse_prefill_pipelined that span many
  * launches: everything up to the end of layer 0 (input rows, re-alignment, the full first layer), and
  * the selective layers 1 .. L-1 with the final copy. */
 enum { CB_PROF_GEMM = 0, CB_PROF_ATTN = 1, CB_PROF_REALIGN = 2, CB_PROF_DEV = 3,

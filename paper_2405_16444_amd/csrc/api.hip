@@ -1048,6 +1048,7 @@ int cb_qkv_norm_rope(cb_ctx *c, const void *q, int64_t q_stride, const void *k, 
   if (!c) return CB_ENULL;
   if (n_rows < 0 || n_cache_rows < 0) return CB_EINVAL;
   if (n_rows == 0) return CB_OK;
+  if (n_rows >= 1 << 24) return CB_EUNSUPPORTED;       // a launch numbers its threads with 32 bits, 256 to a row
   if (!q || !k || !v || !row_pos || !cache_row || !q_out || !k_cache || !v_cache) return CB_ENULL;
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_norm, 16) || !aligned(k_norm, 16) ||
       !aligned(row_pos, 4) || !aligned(cache_row, 4) || !aligned(q_out, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16))
@@ -1071,7 +1072,8 @@ namespace {
 bool plan_shared(const cb_ctx *c, int n_groups, int n_seqs, int n_q, int max_ctx, int tail_stride, SharedAttn *a) {
   const cb_model_desc &m = c->m;
   const int64_t rows = (int64_t)n_groups * n_seqs;
-  if (rows > (1 << 24) || rows * n_q > (1 << 24) || rows * n_q * m.n_q_heads > (1 << 28)) return false;
+  // a launch numbers its threads with 32 bits, at most 256 to a query
+  if (rows > (1 << 23) || rows * n_q > (1 << 23) || rows * n_q * m.n_q_heads > (1 << 23)) return false;
   *a = SharedAttn();
   a->dtype = m.dtype; a->hq = m.n_q_heads; a->hkv = m.n_kv_heads; a->dh = m.head_dim;
   a->n_groups = n_groups; a->n_seqs = n_seqs; a->n_q = n_q; a->tail_stride = tail_stride;
@@ -1182,7 +1184,7 @@ int cb_beam_reorder(cb_ctx *c, void *const *k_tail_layers, void *const *v_tail_l
     return CB_EINVAL;
   for (int l = layer_begin; l < layer_end; ++l) {
     if (!k_tail_layers[l] || !v_tail_layers[l]) return CB_ENULL;
-    if (!aligned(k_tail_layers[l], 16) || !aligned(v_tail_layers[l], 16)) return CB_EINVAL;
+    if (!aligned(k_tail_layers[l], 16) || !aligned(v_tail_layers[l], 16) || k_tail_layers[l] == v_tail_layers[l]) return CB_EINVAL;
   }
   if (!aligned(parent, 4) || !aligned(seq_len, 4)) return CB_EINVAL;
   if (n_beams > kReorderBeams || n_groups > 65535) return CB_EUNSUPPORTED;

@@ -142,7 +142,8 @@ __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__re
   const bool valid = m_own < n_flat;
   const int r_own = (valid ? m_own : n_flat - 1) / g, j_own = (valid ? m_own : n_flat - 1) - r_own * g;
   auto pos_of = [&](int r) { return SHARED ? (q_pos[r] < 0 ? -1 : all_pos) : q_pos[r]; };
-  const int my_pos = valid ? pos_of(r_own) : -1;
+  int my_pos = valid ? pos_of(r_own) : -1;
+  if (SHARED && __any(my_pos >= 0)) my_pos = all_pos;    // padding beside real rows is computed as they are, for nobody: no masking for it
   const long q_off = ((long)(row0 + r_own) * n_q_heads + kvh * g + j_own) * DH;
   bf16x8 qf[NST];
   {

@@ -80,8 +80,8 @@ __global__ __launch_bounds__(256) void qkv_norm_rope_kernel(QkvRows a) {
 // ---------------------------------------------------------------------------
 // Beam selection.  score(beam, token) = scores[beam] + logit - log sum exp(logits of the beam); the order is by score, then lower beam,
 // then larger logit, then lower token.  Within a beam the order is that of the logits, so that a first launch can keep
-// the best of every stretch of a row without knowing its sum; it reads every logit once.  Scores are compared in double:
-// two beams' scores are seldom closer than 1e-7 of each other, the float resolution, but they are not never.
+// the best of every stretch of a row without knowing its sum; it reads every logit once.  Scores are compared in double: as
+// floats, two continuations a float step apart would count as equal or not by the rounding of a sum.
 // ---------------------------------------------------------------------------
 constexpr int BS_PER = 32;                 // logits per lane and round
 constexpr int BS_CAP = 256;                // candidates a wavefront holds
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(BF_THREADS) void beam_final_kernel(BeamSelect a, Be
     if (lane == 0) {
       s_lse[b] = (double)base + log((double)s);
       s_state[b] = done ? 2 : m == INFINITY;
-      s_score[b] = (double)score;
+      s_score[b] = fabsf(score) < INFINITY ? (double)score : -(double)INFINITY;      // not finite: a beam that is not there
     }
   }
   if (tid == 0) s_n = 0;
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(BF_THREADS) void beam_final_kernel(BeamSelect a, Be
     unsigned long long so[BF_PER], best = 0;
 #pragma unroll
     for (int j = 0; j < BF_PER; ++j) {
-      so[j] = 0;                           // no continuation (also one whose score would be -infinity or NaN)
+      so[j] = 0;                           // no continuation
       if (e0 + j * BF_THREADS < entries) {
         const bool first = beam[j] >= 0 && (beam[j] & 0x10000);
         const bool real = beam[j] >= 0;

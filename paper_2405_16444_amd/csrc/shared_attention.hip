@@ -89,6 +89,40 @@ __device__ __forceinline__ int max16(int v) {
   return v;
 }
 
+// First slot of a query's context pieces in a wide launch, and how many pieces its group's context has
+__device__ __forceinline__ size_t wide_slot(const SharedAttn &a, int row, int kvh, int j, int *n) {
+  const int grp = (int)a.by_group_rows.div(row), r0 = row - grp * (int)a.by_group_rows.d;
+  *n = ((a.ctx_len[grp] + 63) / 64 + a.split_tiles - 1) / a.split_tiles;
+  return (((size_t)grp * a.hkv + kvh) * a.ctx_rows + (size_t)r0 * a.g + j) * a.ctx_pieces;
+}
+
+// The end of a query in a launch that folds: joins the context's pieces to the tail's part (top, l, acc: NC blocks of 4 channels from
+// channel ch on, 16 apart) and writes the result.
+template <int NC, int DH>
+__device__ __forceinline__ void fold_and_store(const SharedAttn &a, int row, int kvh, int j, int ch, float top, float l, f32x4 *acc) {
+  int n;
+  const size_t slot0 = wide_slot(a, row, kvh, j, &n);
+  if (a.row_tail[row] < 0) n = 0;
+  for (int p = 0; p < n; ++p) {
+    const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + (slot0 + p) * 2);
+    const float nt = fmaxf(top, ml.x), ref = nt == -INFINITY ? 0.f : nt;
+    const float w0 = __builtin_amdgcn_exp2f(top - ref), w1 = __builtin_amdgcn_exp2f(ml.x - ref);
+    const float *src = a.part_o + (slot0 + p) * DH + ch;
+    top = nt;
+    l = l * w0 + w1 * ml.y;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] = acc[c] * w0 + w1 * *reinterpret_cast<const f32x4 *>(src + 16 * c);
+  }
+  const bool none = l == 0.f || a.row_tail[row] < 0;
+  const float inv = none ? 0.f : 1.f / l;
+  bf16 *dst = (bf16 *)a.o + ((size_t)row * a.hq + kvh * a.g + j) * DH + ch;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const f32x4 v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[c] * inv;
+    store4<bf16>(dst + 16 * c, v[0], v[1], v[2], v[3]);
+  }
+}
+
 // a piece without keys: the merge passes it over
 __device__ __forceinline__ void store_empty(const SharedAttn &a, const Item &it, int tid) {
   for (int qi = tid; it.m0 + qi < it.m_end; qi += blockDim.x) {
@@ -146,7 +180,7 @@ __global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16
   const int n_tiles = (kv_len + SA_TILE - 1) / SA_TILE;
   const int per = (int)(it.tail ? a.by_tail_pieces : a.by_ctx_pieces).div(n_tiles + pieces - 1);
   const int t_begin = piece * per, t_end = min(n_tiles, t_begin + per);
-  if (t_begin >= t_end) {
+  if (t_begin >= t_end && !a.fold) {
     store_empty(a, it, tid);
     return;
   }
@@ -340,6 +374,7 @@ __global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16
   float *dst = a.part_o + slot * DH + 4 * h;
   if constexpr (KS == 1) {
     if (m >= it.m_end) return;
+    if (a.fold) return fold_and_store<NCB, DH>(a, it.row0 + r, kvh, m - r * g, 4 * h, top, row_sum, oacc);
     if (h == 0) *reinterpret_cast<float2 *>(a.part_ml + slot * 2) = make_float2(top, row_sum);
 #pragma unroll
     for (int c = 0; c < NCB; ++c) *reinterpret_cast<f32x4 *>(dst + 16 * c) = oacc[c];
@@ -375,6 +410,7 @@ __global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16
         acc[c] = s == 0 ? w * v : acc[c] + w * v;
       }
     }
+    if (a.fold) return fold_and_store<CPW, DH>(a, it.row0 + r, kvh, m - r * g, 16 * ks * CPW + 4 * h, top, l, acc);
     if (h == 0 && ks == 0) *reinterpret_cast<float2 *>(a.part_ml + slot * 2) = make_float2(top, l);
 #pragma unroll
     for (int c = 0; c < CPW; ++c) *reinterpret_cast<f32x4 *>(dst + 16 * (ks * CPW + c)) = acc[c];
@@ -552,9 +588,7 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedAttn a) {
   size_t slot0 = m * a.ctx_pieces;
   int n_ctx = a.ctx_pieces;
   if (a.wide) {                            // slots by group, only as many pieces as the group's context has
-    const int grp = (int)a.by_group_rows.div(r), r0 = r - grp * (int)a.by_group_rows.d;
-    slot0 = (((size_t)grp * a.hkv + kvh) * a.ctx_rows + (size_t)r0 * g + (hd - kvh * g)) * a.ctx_pieces;
-    n_ctx = ((a.ctx_len[grp] + 63) / 64 + a.split_tiles - 1) / a.split_tiles;
+    slot0 = wide_slot(a, r, kvh, hd - kvh * g, &n_ctx);
   }
   const int n = real ? n_ctx + a.tail_pieces : 0;
   float top = -INFINITY, l = 0.f;
@@ -665,7 +699,7 @@ int tiles_at_a_time(int dtype, int qb) { return dtype == 0 ? SF_NW : qb <= 2 ? 4
 
 }  // namespace
 
-// Pieces: as many workgroups as there are CUs, no piece shorter than the tiles a workgroup takes at a time.  Tails are
+// Pieces: as many workgroups as the chip holds at a time, no piece shorter than the tiles a workgroup takes at a time.  Tails are
 // short as a rule, and how long is not known here, only how long they can be: a piece per 512 rows, within half of the workgroups.
 static void plan(SharedAttn &a, int max_ctx, bool may_wide, bool must_wide) {
   const int g = a.g = a.hq / a.hkv;
@@ -679,6 +713,7 @@ static void plan(SharedAttn &a, int max_ctx, bool may_wide, bool must_wide) {
   // 23 / 48 against 31 / 37.  Every group is a launch, so several groups have to be worth it each.
   a.wide = may_wide && a.dtype != 0 && max_ctx > 0 && ctx_q > 48 &&
            (must_wide || (double)ctx_q * max_ctx >= (a.n_groups == 1 ? 1.6e6 : 4e6));
+  a.fold = 0;
   if (a.wide) a.qb = query_blocks(a.dtype, tail_q);
   const int qpb = 16 * a.qb, step = SA_TILE * tiles_at_a_time(a.dtype, a.qb);
   a.ctx_blocks = (int)((ctx_q + qpb - 1) / qpb);
@@ -692,8 +727,13 @@ static void plan(SharedAttn &a, int max_ctx, bool may_wide, bool must_wide) {
     a.ctx_rows = a.n_qwg * 256;
     a.ctx_items = 0;
     a.tail_slot0 = (size_t)a.n_groups * a.hkv * a.ctx_rows * a.ctx_pieces;
+    a.fold = a.tail_pieces == 1 && a.ctx_pieces <= 2;    // 16 x 64 queries over 4064 tokens: 24 + 14 us for tails and merge -> 27
   } else {
-    const long left = std::max(kSlots / 2, kSlots - tail_units * a.tail_pieces), most = (max_ctx + step - 1) / step;
+    // A piece leaves 520 bytes per query for 512 bytes per key that it reads (dh = 128), written and read again: four keys to a query, up to 256.
+    // 64 queries a key/value head over 3136 keys: 14.9 us without this, 10.8 with it; 128 queries 14.9 + 5.8 for the merge against 15.8 + 4.0
+    // (with four keys to each of the 128: 18.8 + 4.0).
+    const long least = std::max<long>(step, std::min<long>(4 * std::min<long>(ctx_q, qpb), 256));
+    const long left = std::max(kSlots / 2, kSlots - tail_units * a.tail_pieces), most = (max_ctx + least - 1) / least;
     a.ctx_pieces = max_ctx == 0 ? 0 : (int)std::max<long>(1, std::min<long>(most, left / ctx_units));
     a.ctx_items = a.n_groups * a.ctx_blocks * a.ctx_pieces;
     a.tail_slot0 = (size_t)a.rows * a.hq * a.ctx_pieces;
@@ -750,6 +790,7 @@ hipError_t launch_shared_attention(SharedAttn a, float *scratch, hipStream_t s) 
     }
     if (e != hipSuccess) return e;
   }
+  if (a.fold) return hipSuccess;
   if (a.dtype == 0) return a.dh == 64 ? launch_merge<float, 64>(a, s) : launch_merge<float, 128>(a, s);
   return a.dh == 64 ? launch_merge<bf16, 64>(a, s) : launch_merge<bf16, 128>(a, s);
 }

@@ -74,23 +74,26 @@ def rope(x, pos, gain, m):
 
 
 def beam_scores(logits, scores, finished=None, end_token=0):
-    """Scores of every continuation, float64 [rows, vocab], from the definition: NaN logits are -infinity, infinite ones share."""
+    """Scores of every continuation, float64 [rows, vocab], from the definition: NaN logits are -infinity, infinite ones share, a beam
+    whose score is not finite is not there."""
     x = logits.double().nan_to_num(nan=-math.inf, posinf=math.inf, neginf=-math.inf)
     s = scores.double()
     out = torch.full_like(x, -math.inf)
     for r in range(x.shape[0]):
+        if not math.isfinite(float(s[r])):
+            continue
         if finished is not None and int(finished[r]) != 0:
             out[r, end_token] = s[r]
             continue
         m = float(x[r].max())
-        if m == -math.inf or torch.isnan(s[r]):
+        if m == -math.inf:
             continue
         if m == math.inf:
             top = x[r] == math.inf
             out[r, top] = s[r] - math.log(int(top.sum()))
         else:
             out[r] = s[r] + (x[r] - (m + torch.exp(x[r] - m).sum().log()))
-    return out.nan_to_num(nan=-math.inf, posinf=math.inf, neginf=-math.inf)
+    return out
 
 
 def best(all_scores, n_groups, n_keep):

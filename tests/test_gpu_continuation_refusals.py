@@ -38,6 +38,7 @@ def test_norm_rope_refusals(env):
         assert call(f, good, **{name: None}) == ENULL, name
     for name in ("q", "k", "v", "qn", "kn", "out", "kc", "vc"):
         assert call(f, good, **{name: p + 8}) == EINVAL, name
+    assert call(f, good, n=1 << 24) == EUNSUPPORTED
     for bad in (dict(pos=p + 2), dict(row=p + 1), dict(n=-1), dict(rows=-1), dict(qs=248), dict(ks=127), dict(vs=120), dict(qs=257), dict(ks=132)):
         assert call(f, good, **bad) == EINVAL, bad
 
@@ -56,7 +57,7 @@ def test_attention_refusals(env):
                 dict(lens=(C.c_int32 * 2)(5, -1))):
         assert call(f, good, **bad) == EINVAL, bad
     assert call(f, good, size=size - 1) == EWORKSPACE
-    assert call(f, good, n=1 << 22, nq=1 << 22) == EUNSUPPORTED and call(f, good, n=1 << 30) == EUNSUPPORTED
+    assert call(f, good, n=1 << 22, nq=1 << 22) == EUNSUPPORTED and call(f, good, n=1 << 30) == EUNSUPPORTED and call(f, good, g=1, n=(1 << 21) + 1) == EUNSUPPORTED
     for bad in ((0, 1, 1, 5, 5), (1, 0, 1, 5, 5), (1, 1, 0, 5, 5), (1, 1, 1, -1, 5), (1, 1, 1, 5, -1), (1 << 20, 1 << 20, 1, 5, 5)):
         assert P.cb_shared_prefix_workspace_bytes(ctx, *bad) == 0, bad
     assert lib.cb_shared_prefix_workspace_bytes(None, 1, 1, 1, 1, 1) == 0
@@ -91,12 +92,13 @@ def test_select_refusals(env):
 def test_reorder_refusals(env):
     P, lib, ctx, buf = env
     p = buf.data_ptr()
-    ptrs = (C.c_void_p * 3)(p, p, p)
-    good = dict(ctx=ctx._h, k=ptrs, v=ptrs, l0=0, l1=3, g=2, b=4, ts=8, parent=p, len=None, s=None)
+    ptrs, others = (C.c_void_p * 3)(p, p, p), (C.c_void_p * 3)(p + 64, p + 64, p + 64)
+    good = dict(ctx=ctx._h, k=ptrs, v=others, l0=0, l1=3, g=2, b=4, ts=8, parent=p, len=None, s=None)
     f = lib.cb_beam_reorder
     for name in ("ctx", "k", "v", "parent"):
         assert call(f, good, **{name: None}) == ENULL, name
-    assert call(f, good, k=(C.c_void_p * 3)(p, None, p)) == ENULL and call(f, good, v=(C.c_void_p * 3)(p, p, p + 4)) == EINVAL
+    assert call(f, good, k=(C.c_void_p * 3)(p, None, p)) == ENULL and call(f, good, v=(C.c_void_p * 3)(p + 64, p + 64, p + 4)) == EINVAL
+    assert call(f, good, v=ptrs) == EINVAL                                            # K and V of a layer in one array
     assert call(f, good, k=(C.c_void_p * 3)(p, None, p), l0=2) == OK                # layers outside the range are not looked at
     for bad in (dict(l0=-1), dict(l1=4), dict(l0=2, l1=1), dict(g=0), dict(b=0), dict(ts=-1), dict(parent=p + 2), dict(len=p + 1)):
         assert call(f, good, **bad) == EINVAL, bad

@@ -98,6 +98,42 @@ def test_attention_many_query_rows(P, dtype):
     check_attention(P, m, [350], 1, 1, 3000, [2999], 4)
 
 
+WIDE = [  # enough queries and keys for the launch that takes 32 queries per wavefront: one, two and many pieces, one token and many
+    (16, 8, 64, [500], 8, 256, 300), (16, 2, 128, [1111, 1999], 3, 200, 250), (64, 2, 64, [13001], 4, 1, 40), (24, 4, 128, [7001], 41, 1, 33),
+    (16, 2, 64, [5000], 5, 9, 700)]
+
+
+@pytest.mark.parametrize("hq,hkv,dh,plens,n_seqs,n_q,stride", WIDE)
+def test_attention_wide(P, hq, hkv, dh, plens, n_seqs, n_q, stride):
+    m, rt, rng = U.model(hq, hkv, dh, "bf16"), [], random.Random(n_q)
+    for _ in range(len(plens) * n_seqs):
+        new, before = rng.randint(max(1, n_q // 2), n_q), rng.randint(0, stride - n_q)
+        rt += [before + i + 1 if i < new else -1 for i in range(n_q)]
+    rt[0] = 0
+    check_attention(P, m, plens, n_seqs, n_q, stride, rt, n_q, pstride=max(plens) + 5)
+
+
+@pytest.mark.parametrize("hq,hkv,dh,plens,n_seqs,n_q,stride", WIDE[:1] + WIDE[3:])
+def test_attention_wide_hidden_rows_have_no_influence(P, hq, hkv, dh, plens, n_seqs, n_q, stride):
+    m = U.model(hq, hkv, dh, "bf16")
+    rt = [(5 + i if i < n_q - n_q // 3 else -1) for _ in range(n_seqs) for i in range(n_q)]
+    q, kp, vp, kt, vt, r = attention_case(m, plens, n_seqs, n_q, stride, rt, 22, pstride=max(plens) + 70)
+    announce("wide shared attention, hidden rows", hq, hkv, dh, plens, n_seqs, n_q)
+    ctx = P.cb_create(m, 8)
+    ref = call_attention(P, ctx, q, kp, vp, plens, kt, vt, r, n_seqs, n_q)
+    seen = [max(v for v in rt[s * n_q:(s + 1) * n_q]) for s in range(n_seqs)]
+    kp[0, plens[0]:], vp[0, plens[0]:] = NAN, INF
+    for s in range(n_seqs):
+        kt[s, seen[s]:], vt[s, seen[s]:] = INF, NAN
+    kt[1, :], vt[1, :] = NAN, NAN          # all of one continuation's tail: the others do not notice
+    out = call_attention(P, ctx, q, kp, vp, plens, kt, vt, r, n_seqs, n_q)
+    mine = torch.zeros(len(rt), dtype=torch.bool)
+    mine[n_q:2 * n_q] = True
+    assert same(out[~mine], ref[~mine])
+    assert bool(out[mine][torch.tensor(rt)[mine] >= 0].isnan().all()) and not bool(out[mine][torch.tensor(rt)[mine] < 0].any())
+    P.cb_destroy(ctx)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_more_groups_than_one_launch_numbers(P, dtype):
     m = U.model(2, 1, 64, dtype)
@@ -345,6 +381,8 @@ def test_select_ties_go_to_the_lower_beam_then_the_lower_token(P, select_ctx, dt
         x = torch.full((4, 5000), fill, dtype=dt)
         x[:, 1::3] = abs(fill) if fill else -fill              # +0 and -0 are equal
         check_select(P, select_ctx, x.cuda(), torch.zeros(4, device="cuda"), 2, keep)
+    x = torch.zeros((8, 9000), dtype=dt)                       # more equal continuations than the lists hold
+    check_select(P, select_ctx, x.cuda(), torch.zeros(8, device="cuda"), 1, keep)
     x = U.normal((3, 9000), 3, dt, 1.0).round()                # few distinct values, identical beams
     x[1:] = x[0]
     check_select(P, select_ctx, x.cuda(), torch.zeros(3, device="cuda"), 1, keep)
@@ -365,7 +403,7 @@ def test_select_values_that_are_not_finite(P, select_ctx, dtype):
     x[5, :] = torch.finfo(x.dtype).min                         # a mask of the type's lowest value
     x[5, 17] = 0.5
     x[6, 0] = -INF
-    scores = torch.tensor([0.0, -1.0, 0.0, -2.0, -3.0, -30.0, -INF, NAN])
+    scores = torch.tensor([0.0, -1.0, 0.0, -2.0, -3.0, -30.0, INF, NAN])
     for keep in (1, 6, 64):
         for rows in ([0, 1, 2, 3], [3, 4, 5, 6], [0, 2, 6, 7], [7, 5, 4, 1], [1, 1, 1, 1]):
             check_select(P, select_ctx, x[rows].cuda(), scores[rows].cuda(), 1, keep)
