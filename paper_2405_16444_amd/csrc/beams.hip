@@ -534,9 +534,12 @@ hipError_t launch_beam_reorder(void *const *k_layers, void *const *v_layers, int
     const int nl = std::min(kReorderLayers, n_layers - l0);
     ReorderArgs a;
     for (int i = 0; i < 2 * kReorderLayers; ++i) a.layer[i] = (i & 1 ? v_layers : k_layers)[l0 + std::min(i / 2, nl - 1)];
-    // as many workgroups as the slab has work for; a few thousand in all are enough, the rest is walked
+    // Whole slabs would need `need` workgroups each, tails fill them in part: small arrays take as many workgroups as the chip holds at a time (64
+    // slabs of 24 of 128 rows 8.4 us, with 4096 workgroups 10.4), large ones enough to keep it busy to the end (640 of 80 of 96 rows
+    // 261 us with 16384, 279 with 4096).
     const long need = ((long)tail_stride * chunks + 255) / 256, others = (long)n_groups * nl * 2;
-    const dim3 grid((unsigned)std::max<long>(1, std::min<long>(need, 16384 / others)), n_groups, 2 * nl);
+    const long most = need * others <= 8192 ? 2048 : 16384;
+    const dim3 grid((unsigned)std::max<long>(1, std::min<long>(need, most / others)), n_groups, 2 * nl);
 #define CB_REORDER(NB) hipLaunchKernelGGL(beam_reorder_kernel<NB>, grid, dim3(256), 0, s, a, n_beams, tail_stride, chunks, parent, seq_len)
     if (n_beams <= 4) CB_REORDER(4);
     else if (n_beams <= 8) CB_REORDER(8);
