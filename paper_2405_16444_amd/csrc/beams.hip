@@ -14,6 +14,7 @@ namespace {
 // row, so that the position, and with it the (cos, sin) values a lane needs, are the same for all of the heads it walks
 // through.  A lane holds the 16-byte vectors at channel p N and dh/2 + p N of a head: both rotary orders then find their
 // pairs within the lane, the adjacent one inside each vector, the half-split one across the two.
+// 4099 rows of 64 + 2 x 8 heads of 128 with norms 33.7 us = 5.0 TB/s, the rate of a copy; 8 rows 3.3 us, an empty launch being 2.6.
 // ---------------------------------------------------------------------------
 template <typename T, int DH, bool HALF>
 __global__ __launch_bounds__(256) void qkv_norm_rope_kernel(QkvRows a) {
@@ -118,6 +119,7 @@ __device__ __forceinline__ void wave_sync() {
 // (a subtraction, a product, an exponential, an addition), and one comparison with the threshold.  The threshold comes from the first
 // round: n_keep lanes have maxima at or above the n_keep-th largest of the lanes' maxima, so nothing below it is wanted.  What passes it goes to a list that is ranked at the end, or when it is half full, which
 // tightens the threshold; where it overflows (many equal logits), the n_keep-th of those at hand does, and the round is gone through again.
+// 256 rows of 64000 floats 17.2 us = 3.8 TB/s, 4 rows of 32000 6.2 us.
 template <typename TL>
 __global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScratch w) {
   using V = Vec16<TL>;
@@ -258,6 +260,7 @@ __global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScra
 // n_keep-th largest of these is at or below n_keep entries and so a bound, and what reaches it (as a rule one to four times n_keep) is ranked by
 // counting, several threads to an entry.  Entries are numbered by depth in their list, then stretch, then beam, so that each
 // group of threads sees every beam.
+// 6.2 us for 4 beams of 16 stretches and n_keep = 8, 7.9 for 8 beams of 16 and 16.
 struct Cand { unsigned long long score, key; int beam; };      // score: order-preserving image of the double
 __device__ __forceinline__ unsigned long long ord64(double v) {
   const unsigned long long u = (unsigned long long)__double_as_longlong(v + 0.0);
@@ -454,6 +457,7 @@ BeamScratch beam_scratch(int rows, int vocab, int n_keep, void *base, size_t *by
 // ---------------------------------------------------------------------------
 // Reordering in place.  Every 16-byte piece of a row is moved between the beams of its group by one lane, which reads what all of them will
 // receive before it writes any of it: no second buffer, no order between workgroups.  A beam that stays where it is moves nothing.
+// 640 slabs of 80 rows of 2 KB 261 us = 5.0 TB/s, the rate of a copy.
 // ---------------------------------------------------------------------------
 constexpr int kReorderLayers = 128;
 struct ReorderArgs {

@@ -111,6 +111,11 @@ def test_attention_wide(P, hq, hkv, dh, plens, n_seqs, n_q, stride):
         rt += [before + i + 1 if i < new else -1 for i in range(n_q)]
     rt[0] = 0
     check_attention(P, m, plens, n_seqs, n_q, stride, rt, n_q, pstride=max(plens) + 5)
+    q, kp, vp, kt, vt, r = attention_case(m, plens, n_seqs, n_q, stride, rt, n_q, max(plens) + 5)
+    ctx = P.cb_create(m, 8)
+    ref = call_attention(P, ctx, q, kp, vp, plens, kt, vt, r, n_seqs, n_q)
+    assert same(call_attention(P, ctx, q, kp, vp, plens, kt, vt, r, n_seqs, n_q, out=q), ref)      # over the queries
+    P.cb_destroy(ctx)
 
 
 @pytest.mark.parametrize("hq,hkv,dh,plens,n_seqs,n_q,stride", WIDE[:1] + WIDE[3:])
