@@ -272,7 +272,8 @@ int cb_first_token(cb_ctx *ctx, const float *final_hidden, int32_t n_suffix, con
  * continuations of one request.  A decoding step of a layer projects Q, K and V of the new tokens, then calls
  * cb_qkv_norm_rope and cb_shared_prefix_attention; after the last layer come the vocabulary projection, cb_beam_select and,
  * for all layers at once, cb_beam_reorder.  Lengths that change from step to step are device arrays, so that a step
- * can be captured into a graph once.  Needs a stream of the device the ctx was created on (else CB_EINVAL), as cb_first_token. */
+ * can be captured into a graph once.  Nothing is kept in a workspace from one call to the next; calls that overlap in time need one each.
+ * Needs a stream of the device the ctx was created on (else CB_EINVAL), as cb_first_token. */
 
 /* Queries and keys of new tokens: per-head RMSNorm (eps = desc.rms_eps; left out where its gain is NULL), rotation by the token's
  * position in the ctx's rotary order (Appendix A), rounded once after both; the rotated keys and the values go into the cache.

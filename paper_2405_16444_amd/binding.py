@@ -450,6 +450,14 @@ def _fits(ctx: Context, t: torch.Tensor, dtype, shape) -> bool:
     return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == ctx.device.index
 
 
+def _empty(ctx: Context, stream, shape, dtype) -> torch.Tensor:
+    """A tensor of the current stream's that `stream` (None: the current one) uses: not handed out again before that stream is done"""
+    t = torch.empty(shape, dtype=dtype, device=ctx.device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
 def _cache_rows(ctx: Context, k: torch.Tensor, v: torch.Tensor) -> int:
     """Rows of a K and a V array [rows, Hkv, dh], checked"""
     shape = (k.shape[0], ctx.model.n_kv_heads, ctx.model.head_dim)
@@ -482,7 +490,7 @@ def cb_qkv_norm_rope(ctx: Context, qkv, row_pos: torch.Tensor, cache_row: torch.
     assert k_norm is None or _fits(ctx, k_norm, dt, (dh,))
     cache_rows = _cache_rows(ctx, k_cache, v_cache)
     if q_out is None:
-        q_out = torch.empty((n_rows, hq, dh), dtype=dt, device=ctx.device)
+        q_out = _empty(ctx, stream, (n_rows, hq, dh), dt)
     else:
         assert _fits(ctx, q_out, dt, (n_rows, hq, dh))
     status = _lib.cb_qkv_norm_rope(ctx._h, q, qs, k, ks, v, vs, None if q_norm is None else q_norm.data_ptr(),
@@ -511,12 +519,11 @@ def cb_shared_prefix_attention(ctx: Context, q: torch.Tensor, n_groups: int, n_s
     tail_stride, rest_tail = divmod(_cache_rows(ctx, k_tail, v_tail), seqs)
     assert rest == 0 and rest_tail == 0
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(ctx, stream, shape, ctx.dtype)
     else:
         assert _fits(ctx, out, ctx.dtype, shape)
     if workspace is None:
-        workspace = torch.empty(cb_shared_prefix_workspace_bytes(ctx, n_groups, n_seqs, n_q, max(prefix_lens), tail_stride),
-                                dtype=torch.uint8, device=ctx.device)
+        workspace = _empty(ctx, stream, cb_shared_prefix_workspace_bytes(ctx, n_groups, n_seqs, n_q, max(prefix_lens), tail_stride), torch.uint8)
     status = _lib.cb_shared_prefix_attention(ctx._h, q.data_ptr(), n_groups, n_seqs, n_q, k_prefix.data_ptr(), v_prefix.data_ptr(),
                                              (C.c_int32 * n_groups)(*prefix_lens), prefix_stride, k_tail.data_ptr(), v_tail.data_ptr(),
                                              tail_stride, row_tail.data_ptr(), out.data_ptr(), workspace.data_ptr(),
@@ -542,14 +549,13 @@ def cb_beam_select(ctx: Context, logits: torch.Tensor, scores: torch.Tensor, n_g
     shape = (n_groups, n_keep)
     if out is None:
         # beams and tokens lie side by side: one allocation
-        ints = torch.empty((2, n_groups, n_keep), dtype=torch.int32, device=ctx.device)
-        out = (torch.empty(shape, dtype=torch.float32, device=ctx.device), ints[0], ints[1])
+        beams, tokens = _empty(ctx, stream, (2, n_groups, n_keep), torch.int32).unbind(0)
+        out = (_empty(ctx, stream, shape, torch.float32), beams, tokens)
     else:
         assert _fits(ctx, out[0], torch.float32, shape) and _fits(ctx, out[1], torch.int32, shape) and _fits(ctx, out[2], torch.int32, shape)
     n_beams = rows // n_groups
     if workspace is None:
-        workspace = torch.empty(max(256, cb_beam_select_workspace_bytes(ctx, n_groups, n_beams, vocab, n_keep)), dtype=torch.uint8,
-                                device=ctx.device)
+        workspace = _empty(ctx, stream, max(256, cb_beam_select_workspace_bytes(ctx, n_groups, n_beams, vocab, n_keep)), torch.uint8)
     status = _lib.cb_beam_select(ctx._h, logits.data_ptr(), CB_BF16 if half else CB_F32, stride if rows > 1 else vocab, n_groups, n_beams,
                                  vocab, scores.data_ptr(), None if finished is None else finished.data_ptr(), end_token, n_keep,
                                  out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), workspace.data_ptr(), workspace.numel(),

@@ -96,6 +96,7 @@ def test_attention_many_query_rows(P, dtype):
     rt = [40 + i // 2 for _ in range(3) for i in range(150)]
     check_attention(P, m, [900], 3, 150, 600, rt, 3)
     check_attention(P, m, [350], 1, 1, 3000, [2999], 4)
+    check_attention(P, m, [100], 2, 5, 1900, [600, 601, 602, 603, 604, 1895, 1896, 1897, -1, -1], 5)
 
 
 WIDE = [  # enough queries and keys for the launch that takes 32 queries per wavefront: one, two and many pieces, one token and many
@@ -229,6 +230,27 @@ def test_attention_output_over_the_queries_other_streams_and_repetition(P):
         call_attention(P, ctx, over, kp, vp, [777], kt, vt, r, 4, 3, out=over)
     torch.cuda.synchronize()
     assert same(over, ref)
+    P.cb_destroy(ctx)
+
+
+def test_calls_on_a_stream_of_their_own_keep_their_workspaces(P):
+    """workspaces and outputs that the binding allocates are not handed out again while the other stream works on them"""
+    m = U.model(8, 2, 128, "bf16")
+    q, kp, vp, kt, vt, r = attention_case(m, [3000], 6, 1, 50, [1, 2, 3, 10, 11, 50], 52)
+    x = U.normal((24, 20011), 17, std=3.0).cuda()
+    s = U.normal((24,), 18).cuda()
+    ctx = P.cb_create(m, 8)
+    ref, best = call_attention(P, ctx, q, kp, vp, [3000], kt, vt, r, 6, 1), P.cb_beam_select(ctx, x, s, 3, 16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = []
+    for _ in range(10):
+        got.append((call_attention(P, ctx, q, kp, vp, [3000], kt, vt, r, 6, 1, stream=side), P.cb_beam_select(ctx, x, s, 3, 16, stream=side)))
+        junk = [torch.full((1 << 20,), float("nan"), device="cuda") for _ in range(3)]       # takes freed memory on the current stream
+        del junk
+    torch.cuda.synchronize()
+    for out, sel in got:
+        assert same(out, ref) and all(torch.equal(a, b) for a, b in zip(sel, best))
     P.cb_destroy(ctx)
 
 
