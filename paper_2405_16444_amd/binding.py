@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from types import SimpleNamespace
 from typing import Dict, List, Optional, Sequence
 
@@ -88,7 +89,7 @@ def _load():
     lib.cb_beam_select_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
     lib.cb_beam_select_workspace_bytes.restype = sz
     lib.cb_beam_select.argtypes = [vp, vp, i32, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
-    lib.cb_beam_reorder.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), i32, i32, i32, i32, i32, vp, vp, vp]
+    lib.cb_beam_reorder.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp]
     dbl = C.c_double
     lib.cb_recompute_delay.argtypes = [dbl, dbl]
     lib.cb_recompute_delay.restype = dbl
@@ -565,29 +566,30 @@ def cb_beam_select(ctx: Context, logits: torch.Tensor, scores: torch.Tensor, n_g
 
 
 def _layer_ptrs(ctx: Context, layers):
-    """Pointers of per-layer arrays [rows, Hkv, dh]: a sequence of tensors, or one tensor with the layers in front; and their rows."""
+    """Pointers of per-layer arrays [rows, Hkv, dh] (a sequence of tensors, or one tensor with the layers in front) as an array of 64-bit
+    integers, and their rows"""
     m = ctx.model
     if isinstance(layers, torch.Tensor):
         n, rows = layers.shape[:2]
         assert _fits(ctx, layers, ctx.dtype, (n, rows, m.n_kv_heads, m.head_dim))
         base, step = layers.data_ptr(), layers.stride(0) * layers.element_size()
-        return (C.c_void_p * n)(*range(base, base + n * step, step)) if n * step else (C.c_void_p * n)(), n, rows
+        return array("Q", range(base, base + n * step, step) if n * step else (0,) * n), rows
     rows = layers[0].shape[0]
     for t in layers:
         assert _fits(ctx, t, ctx.dtype, (rows, m.n_kv_heads, m.head_dim))
-    return (C.c_void_p * len(layers))(*[t.data_ptr() for t in layers]), len(layers), rows
+    return array("Q", [t.data_ptr() for t in layers]), rows
 
 
 def cb_beam_reorder(ctx: Context, k_tail_layers, v_tail_layers, n_groups: int, parent: torch.Tensor,
                     seq_len: Optional[torch.Tensor] = None, stream=None):
     """The beams' tails follow their parents, in place.  k_tail_layers / v_tail_layers: per layer [n_groups * n_beams * tail_stride, Hkv, dh],
     as a sequence of tensors or one tensor [layers, ...]; at most the model's layers.  parent, seq_len: int32 [n_groups * n_beams]."""
-    k, nk, rows = _layer_ptrs(ctx, k_tail_layers)
-    v, nv, rows_v = _layer_ptrs(ctx, v_tail_layers)
+    k, rows = _layer_ptrs(ctx, k_tail_layers)
+    v, rows_v = _layer_ptrs(ctx, v_tail_layers)
     beams = parent.numel()
-    assert nk == nv and rows == rows_v and n_groups >= 1 and beams >= n_groups and beams % n_groups == 0 and rows % beams == 0
+    assert len(k) == len(v) and rows == rows_v and n_groups >= 1 and beams >= n_groups and beams % n_groups == 0 and rows % beams == 0
     assert _fits(ctx, parent, torch.int32, (beams,)) and (seq_len is None or _fits(ctx, seq_len, torch.int32, (beams,)))
-    status = _lib.cb_beam_reorder(ctx._h, k, v, 0, nk, n_groups, beams // n_groups, rows // beams, parent.data_ptr(),
+    status = _lib.cb_beam_reorder(ctx._h, k.buffer_info()[0], v.buffer_info()[0], 0, len(k), n_groups, beams // n_groups, rows // beams, parent.data_ptr(),
                                   None if seq_len is None else seq_len.data_ptr(), _current_stream(ctx, stream))
     _check(status, "cb_beam_reorder")
 
