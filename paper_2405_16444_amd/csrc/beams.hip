@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void qkv_norm_rope_kernel(QkvRows a) {
 // Beam selection.  score(beam, token) = scores[beam] + logit - log sum exp(logits of the beam); the order is by score, then lower beam,
 // then larger logit, then lower token.  Within a beam the order is that of the logits, so that a first launch can keep
 // the best of every stretch of a row without knowing its sum; it reads every logit once.  Scores are compared in double: as
-// floats, two continuations a float step apart would count as equal or not by the rounding of a sum.
+// floats, different logits of a beam would tie.  The sums of exponentials are float (a relative 1e-7, the same for a whole beam).
 // ---------------------------------------------------------------------------
 constexpr int BS_PER = 32;                 // logits per lane and round
 constexpr int BS_CAP = 256;                // candidates a wavefront holds

@@ -366,10 +366,10 @@ def check_select(P, ctx, logits, scores, n_groups, n_keep, finished=None, end_to
             assert s == ws or abs(s - ws) <= tol, (g, i, s, ws)
             assert (b, t) not in seen and 0 <= b < beams and 0 <= t < vocab
             seen.add((b, t))
-            others = [want[j] for j in (i - 1, i + 1) if j >= 0 and want[j][1] != wb]
-            if all(abs(o[0] - ws) > 2 * tol or o[0] == ws for o in others):
+            rest = torch.cat((every[g * beams:g * beams + wb], every[g * beams + wb + 1:(g + 1) * beams])) - ws
+            if not bool(((rest.abs() <= 2 * tol) & (rest != 0)).any()):
                 assert (b, t) == (wb, wt), (g, i, (s, b, t), want[i])
-            else:                         # two beams nearer to each other than the float sums resolve
+            else:                         # another beam's score is nearer than the float sums of both resolve, and not the same
                 assert abs(float(every[g * beams + b, t]) - ws) <= 2 * tol
 
 
