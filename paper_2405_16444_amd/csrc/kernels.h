@@ -197,6 +197,7 @@ struct SharedAttn {
   int dtype, qb, ctx_blocks, ctx_pieces, tail_blocks, tail_pieces;
   // wide: a launch of its own for the context (attention_context_plan); ctx_rows: queries of a group in its slots' numbering
   int wide, n_qwg, split_tiles, ctx_rows, most_pieces;
+  int stream;                              // the contexts are loaded non-temporally
   int fold;                                // wide: the tails' launch joins the context's partial results and writes o
   FastDiv by_group_rows, by_hq;
 };

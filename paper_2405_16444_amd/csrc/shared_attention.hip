@@ -140,12 +140,14 @@ __device__ __forceinline__ void store_empty(const SharedAttn &a, const Item &it,
 // block, whatever QB.  (With two blocks unrolled in one wavefront eight beams over 3136 keys took 10.0 us instead of 8.7: each
 // instruction of a short piece is executed once, so the time is that of fetching them.)  The QB wavefronts of a tile share its loads;
 // the KS tiles' results are joined in LDS.
-// Eight beams, 32 query heads over 8: 3136 keys 9.0 us, of which the burst of all loads is 2; 32896 keys 32.8 us = 4.3 TB/s.
+// Eight beams, 32 query heads over 8: 3136 keys 9.0 us, of which the burst of all loads is 2; 32896 keys 31.7 us = 4.4 TB/s, 65536
+// keys 56 us = 4.8 TB/s.
 // ---------------------------------------------------------------------------
 constexpr int shared_ring_bytes(int dh, int ks, int st) { return ks * st * 2 * SA_TILE * dh * 2; }
 // RAGGED: several new tokens per continuation (n_q > 1), which see different tail rows and may be padding.  Else everything in the item's range
 // is seen by all of its queries.
-template <int DH, int QB, int KS, int ST, bool RAGGED>
+// NT: keys and values are loaded non-temporally.
+template <int DH, int QB, int KS, int ST, bool RAGGED, bool NT>
 __global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16_kernel(SharedAttn a) {
   constexpr int ROWB = DH * 2, CH = DH / 8, RPI = 1024 / ROWB, TB = SA_TILE * ROWB, LPT = SA_TILE / RPI, LPW = 2 * LPT / QB;
   constexpr int NKS = DH / 32, NCB = DH / 16, NQ = 16 * QB;
@@ -207,7 +209,7 @@ __global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16
       const unsigned col = is_v ? vc ^ (fv(i * RPI) * 16) : kc ^ (fk(i * RPI) * 16);
       const char *src = (is_v ? it.v : it.k) + tile0 + (unsigned)(min((int)(i * RPI + lr), last) * row_bytes + col);
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
-                                       (__attribute__((address_space(3))) void *)(ring + stage * 2 * TB + l * 1024), 16, 0, 0);
+                                       (__attribute__((address_space(3))) void *)(ring + stage * 2 * TB + l * 1024), 16, 0, NT ? 2 : 0);
     }
   };
   const int n_it = (t_end - t_begin + KS - 1) / KS, n_mine = (t_end - t_begin - ks + KS - 1) / KS;
@@ -655,21 +657,26 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedAttn a) {
   store4<T>((T *)a.o + ((size_t)r * a.hq + hd) * DH + c * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
-template <int DH, int QB, int KS, int ST, bool RAGGED>
+template <int DH, int QB, int KS, int ST, bool RAGGED, bool NT = false>
 hipError_t launch_bf16(const SharedAttn &a, unsigned grid, hipStream_t s) {
   constexpr int smem = shared_ring_bytes(DH, KS, ST) + QB * KS * 16 * 8;
   static_assert(shared_ring_bytes(DH, KS, ST) >= QB * KS * (DH / 16) * 1024 || KS == 1, "the join fits in the rings' place");
   static std::once_flag once;
   std::call_once(once, [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&shared_attn_bf16_kernel<DH, QB, KS, ST, RAGGED>),
+    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&shared_attn_bf16_kernel<DH, QB, KS, ST, RAGGED, NT>),
                               hipFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
-  hipLaunchKernelGGL((shared_attn_bf16_kernel<DH, QB, KS, ST, RAGGED>), dim3(grid), dim3(64 * QB * KS), smem, s, a);
+  hipLaunchKernelGGL((shared_attn_bf16_kernel<DH, QB, KS, ST, RAGGED, NT>), dim3(grid), dim3(64 * QB * KS), smem, s, a);
   return hipGetLastError();
 }
 template <int DH>
 hipError_t launch_bf16_qb(const SharedAttn &a, unsigned grid, hipStream_t s) {
   // as many tiles at a time as the wavefronts leave; one new token: two workgroups to a CU, which hide each other's loads
+  if (a.n_q == 1 && a.stream) switch (a.qb) {
+      case 1: return launch_bf16<DH, 1, 4, 1, false, true>(a, grid, s);
+      case 2: return launch_bf16<DH, 2, 4, 1, false, true>(a, grid, s);
+      case 4: return launch_bf16<DH, 4, 2, 2, false, true>(a, grid, s);
+    }
   if (a.n_q == 1) switch (a.qb) {
       case 1: return launch_bf16<DH, 1, 4, 1, false>(a, grid, s);
       case 2: return launch_bf16<DH, 2, 4, 1, false>(a, grid, s);
@@ -768,6 +775,12 @@ hipError_t launch_shared_attention(SharedAttn a, float *scratch, hipStream_t s) 
   a.part_o = scratch;
   a.part_ml = scratch + (a.tail_slot0 + (size_t)a.rows * a.hq * a.tail_pieces) * a.dh;
   a.scale_log2e = kLog2e / sqrtf((float)a.dh);
+  // One query block reads everything once: contexts that the caches will hardly hold until the next step are not kept in them.  Eight beams
+  // over 65536 keys (268 MB) 61 -> 56 us, 32896 keys 33.0 -> 31.7, four beams 30.6 -> 27.2, 28000 keys 25.0 -> 23.6; 20000 keys (82 MB) 21.9 ->
+  // 22.3, 12000 keys 15.2 -> 17.1.
+  double keys = 0;
+  for (int grp = 0; grp < a.n_groups; ++grp) keys += a.ctx_len[grp];
+  a.stream = !a.wide && a.ctx_blocks == 1 && keys * a.hkv * a.dh * 4 >= 96.0 * (1 << 20);
   if (a.wide) {
     const int rows = a.n_seqs * a.n_q;
     const size_t q_row = (size_t)a.hq * a.dh * 2, slab = (size_t)a.ctx_stride * a.hkv * a.dh * 2, slots = (size_t)a.hkv * a.ctx_rows * a.ctx_pieces;

@@ -140,6 +140,14 @@ def test_attention_wide_hidden_rows_have_no_influence(P, hq, hkv, dh, plens, n_s
     P.cb_destroy(ctx)
 
 
+@pytest.mark.parametrize("hq,hkv,dh,plens,n_seqs", [(8, 8, 128, [24641, 100], 3), (32, 8, 128, [25013], 7), (48, 8, 64, [50111], 8)])
+def test_attention_contexts_larger_than_the_caches(P, hq, hkv, dh, plens, n_seqs):
+    """of 100 MB and more: loaded past the caches, one, two and four query blocks"""
+    m, rng = U.model(hq, hkv, dh, "bf16"), random.Random(hq)
+    rt = [rng.randint(-1, 60) for _ in range(len(plens) * n_seqs)]
+    check_attention(P, m, plens, n_seqs, 1, 60, rt, 9, pstride=max(plens) + 3)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_more_groups_than_one_launch_numbers(P, dtype):
     m = U.model(2, 1, 64, dtype)
