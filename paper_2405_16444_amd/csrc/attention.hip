@@ -246,7 +246,7 @@ __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__re
       for (int e = 0; e < 4; ++e) pf[a][u].w[e] = 0u;
 
   bf16x8 kf[4];
-  union VF { s16x4 s[2]; bf16x8 b; } vf[4];
+  union VF { s16x4 s[2]; bf16x8 b; unsigned w[4]; } vf[4];
   // Requests step I of a phase: the K fragment (WK) of k-step I and the V fragment (two transposing reads, WV) of
   // (16-key group I / DB, channel block I % DB).  ODD: the phase works on S of the first half of the next K
   // tile and on the first half of the V tile after the one the addresses point at, so its reads move the
@@ -266,8 +266,9 @@ __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__re
 
   // One phase: softmax of sub-tile j = 2t + ODD (SM), S of sub-tile j+1 (WS), O += V P of sub-tile j-1.
   // NS / NX: whether the phase that follows computes S / exists (its first two steps are requested here).
-  auto phase = [&](auto odd_, auto sm_, auto ws_, auto ns_, auto nx_, int t, int dk, int dv) {
-    constexpr int ODD = decltype(odd_)::value, SM = decltype(sm_)::value, WS = decltype(ws_)::value;
+  // CV: rows of sub-tile j-1 past the end, which repeat the last one, are cleared: their p is 0, but 0 times a value that is not finite is not 0.
+  auto phase = [&](auto odd_, auto sm_, auto ws_, auto ns_, auto nx_, auto cv_, int t, int dk, int dv) {
+    constexpr int ODD = decltype(odd_)::value, SM = decltype(sm_)::value, WS = decltype(ws_)::value, CV = decltype(cv_)::value;
     constexpr int NS = decltype(ns_)::value, NX = decltype(nx_)::value;
     f32x16 &sc = sacc[ODD], &sn = sacc[1 - ODD];
     PF (&pc)[2] = pf[ODD], (&pp)[2] = pf[1 - ODD];
@@ -348,6 +349,13 @@ __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__re
       __builtin_amdgcn_sched_barrier(0);
       vec(IntC<2 * I>{});
       asm volatile("" : "+v"(vf[I & 3].s[0]), "+v"(vf[I & 3].s[1]));
+      if constexpr (CV) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {                  // two adjacent keys a word
+          const int key = t * BKV + (ODD ? 0 : 32) + 16 * (I / DB) + 8 * (w >> 1) + 4 * h + 2 * (w & 1);
+          vf[I & 3].w[w] &= key + 1 < kv_len ? 0xFFFFFFFFu : key < kv_len ? 0xFFFFu : 0u;
+        }
+      }
       oacc[I % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[I & 3].b, pp[I / DB].b, oacc[I % DB], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
       vec(IntC<2 * I + 1>{});
@@ -410,17 +418,30 @@ __global__ __launch_bounds__(64 * ATT_NW) void attn_bf16_kernel(const bf16 *__re
     read_step(IntC<0>{}, IntC<1>{}, IntC<1>{}, IntC<0>{}, 0, 0);
     read_step(IntC<0>{}, IntC<1>{}, IntC<1>{}, IntC<1>{}, 0, 0);
     int dv = 0;
+    // 0 times a stand-in that is not finite has left NaN
+    int first = t_begin;
+    if constexpr (SHARED) asm volatile("" : "+s"(first));     // else the first iteration is compiled as a copy of its own
+    auto clear_first = [&](int at) {
+      if (SHARED && at == first) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) oacc[d][i] = 0.f;
+      }
+    };
     for (; t < t_last; ++t) {
       const int dk = stage_step(t);
-      phase(IntC<0>{}, IntC<1>{}, IntC<1>{}, IntC<1>{}, IntC<1>{}, t, dk, dv);
-      phase(IntC<1>{}, IntC<1>{}, IntC<1>{}, IntC<1>{}, IntC<1>{}, t, dk, dv);
+      phase(IntC<0>{}, IntC<1>{}, IntC<1>{}, IntC<1>{}, IntC<1>{}, IntC<0>{}, t, dk, dv);
+      clear_first(t);
+      phase(IntC<1>{}, IntC<1>{}, IntC<1>{}, IntC<1>{}, IntC<1>{}, IntC<0>{}, t, dk, dv);
       dv = dk;
       att_vm_wait<2 * LPT>();
       asm volatile("s_barrier" ::: "memory");
     }
-    phase(IntC<0>{}, IntC<1>{}, IntC<1>{}, IntC<0>{}, IntC<1>{}, t, 0, dv);
-    phase(IntC<1>{}, IntC<1>{}, IntC<0>{}, IntC<0>{}, IntC<1>{}, t, 0, dv);
-    phase(IntC<0>{}, IntC<0>{}, IntC<0>{}, IntC<0>{}, IntC<0>{}, t, 0, 0);     // O += V P of the last sub-tile
+    phase(IntC<0>{}, IntC<1>{}, IntC<1>{}, IntC<0>{}, IntC<1>{}, IntC<0>{}, t, 0, dv);
+    clear_first(t);
+    phase(IntC<1>{}, IntC<1>{}, IntC<0>{}, IntC<0>{}, IntC<1>{}, IntC<SHARED>{}, t, 0, dv);
+    phase(IntC<0>{}, IntC<0>{}, IntC<0>{}, IntC<0>{}, IntC<0>{}, IntC<SHARED>{}, t, 0, 0);     // O += V P of the last sub-tile
     if (++t < n_tiles) {
       att_vm_wait<2 * LPT>();
       asm volatile("s_barrier" ::: "memory");
