@@ -1071,14 +1071,10 @@ namespace {
 // Fills in the shapes of an attention call and plans it; false: more rows or slots than the launches number.
 bool plan_shared(const cb_ctx *c, int n_groups, int n_seqs, int n_q, int max_ctx, int tail_stride, SharedAttn *a) {
   const cb_model_desc &m = c->m;
-  const int64_t rows = (int64_t)n_groups * n_seqs;
-  // a launch numbers its threads with 32 bits, at most 256 to a query
-  if (rows > (1 << 23) || rows * n_q > (1 << 23) || rows * n_q * m.n_q_heads > (1 << 23)) return false;
   *a = SharedAttn();
   a->dtype = m.dtype; a->hq = m.n_q_heads; a->hkv = m.n_kv_heads; a->dh = m.head_dim;
   a->n_groups = n_groups; a->n_seqs = n_seqs; a->n_q = n_q; a->tail_stride = tail_stride;
-  shared_attention_plan(*a, max_ctx);
-  return true;
+  return shared_attention_plan(*a, max_ctx);
 }
 }  // namespace
 

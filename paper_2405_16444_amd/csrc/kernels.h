@@ -201,8 +201,9 @@ struct SharedAttn {
   int fold;                                // wide: the tails' launch joins the context's partial results and writes o
   FastDiv by_group_rows, by_hq;
 };
-// chooses the pieces for contexts of up to max_ctx rows (from the shapes above alone)
-void shared_attention_plan(SharedAttn &a, int max_ctx);
+// chooses the pieces for contexts of up to max_ctx rows (from the shapes above alone); false, whatever max_ctx: more rows or workgroups
+// than the launches number
+bool shared_attention_plan(SharedAttn &a, int max_ctx);
 // floats of scratch that launches with contexts of up to max_ctx rows need; never falls with max_ctx
 size_t shared_attention_floats(SharedAttn a, int max_ctx);
 hipError_t launch_shared_attention(SharedAttn a, float *scratch, hipStream_t s);

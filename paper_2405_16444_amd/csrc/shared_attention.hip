@@ -757,7 +757,20 @@ static void plan(SharedAttn &a, int max_ctx, bool may_wide, bool must_wide) {
   a.by_tail_blocks = FastDiv(a.tail_blocks);
 }
 
-void shared_attention_plan(SharedAttn &a, int max_ctx) { plan(a, max_ctx, true, false); }
+// A launch numbers its threads with 32 bits.  Of the launches that contexts of any length take, the one that reads contexts and tails has the
+// most (the tails beside a wide one take as many workgroups, of no more threads); the merge has at most 256 to a query and head.  Pieces beyond the
+// first are made only within 512 and 256 workgroups.
+bool shared_attention_plan(SharedAttn &a, int max_ctx) {
+  const long seqs = (long)a.n_groups * a.n_seqs, most = 1 << 23;
+  if (seqs > most || seqs * a.n_q > most || seqs * a.n_q * a.hq > most) return false;
+  const long g = a.hq / a.hkv, ctx_q = (long)a.n_seqs * a.n_q * g, tail_q = a.n_q * g;
+  const int qb = query_blocks(a.dtype, ctx_q), qpb = 16 * qb, threads = 64 * qb * tiles_at_a_time(a.dtype, qb);
+  const long contexts = std::max(a.n_groups * a.hkv * ((ctx_q + qpb - 1) / qpb), 512l);
+  const long tails = a.tail_stride == 0 ? 0 : std::max(seqs * a.hkv * ((tail_q + qpb - 1) / qpb), 256l);
+  if ((contexts + tails) * threads >= 1l << 32) return false;
+  plan(a, max_ctx, true, false);
+  return true;
+}
 
 static size_t floats_of(const SharedAttn &a) {
   const size_t ctx = a.wide ? (size_t)a.n_groups * a.hkv * a.ctx_rows * a.most_pieces : a.tail_slot0;
@@ -811,3 +824,14 @@ hipError_t launch_shared_attention(SharedAttn a, float *scratch, hipStream_t s) 
 }
 
 }  // namespace cb
+
+// The plan of a call with contexts of max_ctx rows, for tests without a device: 1 and what follows, or 0 where it is refused
+extern "C" int cb_internal_shared_plan(int dtype, int hq, int hkv, int dh, int n_groups, int n_seqs, int n_q, int max_ctx, int tail_stride, int *out) {
+  cb::SharedAttn a = cb::SharedAttn();
+  a.dtype = dtype; a.hq = hq; a.hkv = hkv; a.dh = dh;
+  a.n_groups = n_groups; a.n_seqs = n_seqs; a.n_q = n_q; a.tail_stride = tail_stride;
+  if (!cb::shared_attention_plan(a, max_ctx)) return 0;
+  const int v[] = {a.wide, a.fold, a.qb, a.ctx_blocks, a.ctx_pieces, a.tail_blocks, a.tail_pieces};
+  std::copy(v, v + 7, out);
+  return 1;
+}

@@ -107,3 +107,13 @@ def best(all_scores, n_groups, n_keep):
         res.append([(float(a), int(b) // vocab, int(b) % vocab) if a > -math.inf else (-math.inf, -1, -1) for a, b in zip(v, i)] +
                    [(-math.inf, -1, -1)] * (n_keep - len(v)))
     return res
+
+
+def attention_plan(m, n_groups, n_seqs, n_q, prefix, tail_stride):
+    """The launches that cb_shared_prefix_attention chooses, asked of the library without a device; None: refused."""
+    import ctypes
+    from paper_2405_16444_amd.binding import _lib
+    out = (ctypes.c_int * 7)()
+    if not _lib.cb_internal_shared_plan(int(m.dtype == "bf16"), m.n_q_heads, m.n_kv_heads, m.head_dim, n_groups, n_seqs, n_q, prefix, tail_stride, out):
+        return None
+    return SimpleNamespace(**dict(zip(("wide", "fold", "qb", "ctx_blocks", "ctx_pieces", "tail_blocks", "tail_pieces"), out)))

@@ -76,3 +76,15 @@ def test_a_visible_infinity_gives_an_infinity_whatever_the_launch(P, hq, hkv, dh
             assert bool((out[hit] == bad).all()), (rows, bad)
             assert same(out[~hit], ref[~hit]), (rows, bad)
     P.cb_destroy(ctx)
+
+
+def test_more_workgroups_than_a_launch_numbers_are_refused(P):
+    """2^23 tails' heads of 512 threads each: refused before anything is read, as the size query says"""
+    import ctypes as C
+    from paper_2405_16444_amd import binding
+    ctx = P.cb_create(U.model(32, 32, 128, "bf16"), 8)
+    assert P.cb_shared_prefix_workspace_bytes(ctx, 64, 4096, 1, 40, 1) == 0 and P.cb_shared_prefix_workspace_bytes(ctx, 64, 3900, 1, 40, 1) > 0
+    buf = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    p, lens = buf.data_ptr(), (C.c_int32 * 64)(*[40] * 64)
+    assert binding._lib.cb_shared_prefix_attention(ctx._h, p, 64, 4096, 1, p, p, lens, 40, p, p, 1, p, p, p, 1 << 60, None) == -4
+    P.cb_destroy(ctx)

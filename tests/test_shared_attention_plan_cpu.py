@@ -1,0 +1,39 @@
+"""The launches of attention over a shared context, asked of the library's planner without a device."""
+import pytest
+
+import continuation_util as U
+
+
+def threads(m, n_groups, n_seqs, n_q, prefix, stride):
+    """of the launch that reads contexts and tails, from its plan: a work item for every piece of every block of queries and key/value head"""
+    p = U.attention_plan(m, n_groups, n_seqs, n_q, prefix, stride)
+    items = n_groups * n_seqs * p.tail_blocks * p.tail_pieces + (0 if p.wide else n_groups * p.ctx_blocks * p.ctx_pieces)
+    return items * m.n_kv_heads * (256 if p.qb == 1 else 512)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv", [(32, 32), (32, 8), (64, 1), (128, 1), (8, 1), (1, 1)])
+def test_accepted_launches_number_their_threads_with_32_bits(dtype, hq, hkv):
+    m, accepted = U.model(hq, hkv, 128, dtype), 0
+    for groups in (1, 3, 64):
+        for n_q in (1, 2, 64):
+            for shift in range(0, 24):
+                for n_seqs in ((1 << shift) - 1, 1 << shift):
+                    for prefix in (0, 1, 40, 100000):
+                        for stride in (0, 1, 700, 40000):
+                            if n_seqs == 0 or n_seqs * groups * n_q * hq > 1 << 23:
+                                continue
+                            if U.attention_plan(m, groups, n_seqs, n_q, prefix, stride) is None:
+                                assert groups * n_seqs * n_q * hq > 1 << 22
+                            else:
+                                accepted += 1
+                                assert threads(m, groups, n_seqs, n_q, prefix, stride) < 1 << 32
+    assert accepted > 1000
+
+
+def test_the_largest_launch_is_refused():
+    m = U.model(32, 32, 128, "bf16")
+    # a tail of one row, and none: 2^23 key/value heads of 512 threads
+    assert U.attention_plan(m, 64, 4096, 1, 0, 1) is None and U.attention_plan(m, 64, 4096, 1, 40, 1) is None
+    assert U.attention_plan(m, 64, 4096, 1, 40, 0) is not None and U.attention_plan(m, 64, 3900, 1, 40, 1) is not None
+    assert U.attention_plan(m, 64, 4097, 1, 40, 0) is None
