@@ -318,8 +318,9 @@ int cb_shared_prefix_attention(cb_ctx *ctx, const void *q, int32_t n_groups, int
 /* The best continuations of every group: the n_keep largest of
  *     scores[beam] + logits[beam][token] - log sum_t exp(logits[beam][t])
  * over the group's beams and the vocabulary, largest first, equal ones by lower beam, then larger logit, then lower token.  Scores are
- * compared in double, from float sums of the exponentials: within a beam the order is exact, continuations of different beams nearer to each
- * other than about 1e-6 may come in either order (beams with the same logits and scores tie exactly).
+ * compared in double, from sums of exponentials with a relative error of at most (63 + 5 ln vocab) 2^-24 (7.1e-6 at 64000 tokens): within a beam
+ * the order is exact, continuations of different beams nearer to each other than twice that may come in either order (beams with the same
+ * logits and scores tie exactly).
  *   logits    : logits_dtype (cb_dtype, need not be T), row r = group * n_beams + beam at logits + r * row_stride (elements); any
  *               alignment of its type.  NaN counts as -infinity; infinite logits share their beam's probability
  *   scores    : float [n_groups * n_beams], the beams' sums so far; one that is not finite: a beam that is not there

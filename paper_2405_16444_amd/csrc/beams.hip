@@ -82,7 +82,13 @@ __global__ __launch_bounds__(256) void qkv_norm_rope_kernel(QkvRows a) {
 // Beam selection.  score(beam, token) = scores[beam] + logit - log sum exp(logits of the beam); the order is by score, then lower beam,
 // then larger logit, then lower token.  Within a beam the order is that of the logits, so that a first launch can keep
 // the best of every stretch of a row without knowing its sum; it reads every logit once.  Scores are compared in double: as
-// floats, different logits of a beam would tie.  The sums of exponentials are float (a relative 1e-7, the same for a whole beam).
+// floats, different logits of a beam would tie.
+// The sums of exponentials are float within a round of a lane and over the lanes of a wavefront, double over a lane's rounds and stretches, relative to
+// references that move only when a logit exceeds them by 1.  Their relative error, in units of u = 2^-24: 31 additions, 6 levels of lanes twice, 2 for the
+// exponential and for either join's factor, 4 roundings, and for every unit of distance between a logit and the references that it is taken relative to
+// on its way 3 for the exponent (subtraction, product, constant) or 5 (a move is 1 at least: its factor's 2 as well).  Weighted by their
+// probabilities the distances to the maximum average to at most ln vocab, the references' lag adds 2: (63 + 5 ln vocab) u, the same for a
+// whole beam.
 // ---------------------------------------------------------------------------
 constexpr int BS_PER = 32;                 // logits per lane and round
 constexpr int BS_CAP = 256;                // candidates a wavefront holds
@@ -102,7 +108,7 @@ __device__ __forceinline__ unsigned long long lane_value(unsigned long long v, i
 }
 
 struct BeamScratch {
-  float2 *ms;                              // [rows][pieces] maximum and sum of exponentials of a stretch
+  float2 *ms;                              // [rows][pieces] reference of a stretch (infinite as its maximum is) and sum of exponentials relative to it
   unsigned long long *keys;                // [rows][pieces][n_keep] its best logits, descending, 0 behind the last
   FastDiv by_lists, by_beams;              // lists of a group, beams of a group
   int pieces, rounds;                      // stretches of a row, each rounds * 64 * BS_PER logits
@@ -115,7 +121,7 @@ __device__ __forceinline__ void wave_sync() {
 }
 
 // One wavefront: a stretch of a row, 64 x BS_PER logits at a time (the next ones on their way meanwhile would take the registers of the wavefronts
-// that hide the loads).  Bound by HBM where there are many rows, so the instructions per logit count: the running maximum and sum of exponentials, kept per lane and joined at the end
+// that hide the loads).  Bound by HBM where there are many rows, so the instructions per logit count: the running reference and sum of exponentials, kept per lane and joined at the end
 // (a subtraction, a product, an exponential, an addition), and one comparison with the threshold.  The threshold comes from the first
 // round: n_keep lanes have maxima at or above the n_keep-th largest of the lanes' maxima, so nothing below it is wanted.  What passes it goes to a list that is ranked at the end, or when it is half full, which
 // tightens the threshold; where it overflows (many equal logits), the n_keep-th of those at hand does, and the round is gone through again.
@@ -152,7 +158,8 @@ __global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScra
         }
     }
   };
-  float lm = -INFINITY, ls = 0.f, tv = -INFINITY;
+  float ref = -INFINITY, tv = -INFINITY;
+  double ls = 0.0;                         // of exp(logit - ref)
   unsigned long long thr = 0;
   int n = 0;
 #pragma unroll 1
@@ -166,21 +173,22 @@ __global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScra
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < BS_PER; ++i) m = fmaxf(m, x[i]);
-    const float nm = fmaxf(lm, m);
-    if (__any(nm == INFINITY)) {           // infinite logits share the probability: the sum is their number
-      ls = nm == INFINITY && lm == INFINITY ? ls : nm == INFINITY ? 0.f : ls * __builtin_amdgcn_exp2f((lm - (nm == -INFINITY ? 0.f : nm)) * kLog2e);
+    if (__any(m > ref + 1.f)) {
+      const float nr = m > ref + 1.f ? m : ref;
+      ls = nr == ref ? ls : nr == INFINITY ? 0.0 : ls * (double)__builtin_amdgcn_exp2f((ref - nr) * kLog2e);
+      ref = nr;
+    }
+    float part = 0.f;
+    if (__any(ref == INFINITY)) {          // infinite logits share the probability: the sum is their number
 #pragma unroll
       for (int i = 0; i < BS_PER; ++i)
-        ls += nm == INFINITY ? (x[i] == INFINITY ? 1.f : 0.f) : nm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i] - nm) * kLog2e);
+        part += ref == INFINITY ? (x[i] == INFINITY ? 1.f : 0.f) : ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i] - ref) * kLog2e);
     } else {
-      const float base = nm == -INFINITY ? 0.f : nm;
-      ls *= __builtin_amdgcn_exp2f((lm - base) * kLog2e);
-      float part = 0.f;
+      const float base = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
       for (int i = 0; i < BS_PER; ++i) part += __builtin_amdgcn_exp2f((x[i] - base) * kLog2e);
-      ls += part;
     }
-    lm = nm;
+    ls += (double)part;
     if (round == 0) {
       int at_least = 0;                    // lanes whose maximum is no smaller
 #pragma unroll 16
@@ -246,9 +254,9 @@ __global__ __launch_bounds__(64) void beam_stretch_kernel(BeamSelect a, BeamScra
       wave_sync();
     }
   }
-  const float wm = wave_max(lm);
-  // a lane whose maximum is not the infinite one of the row adds nothing to it
-  float sum = wm == INFINITY ? (lm == INFINITY ? ls : 0.f) : wm == -INFINITY ? 0.f : ls * __builtin_amdgcn_exp2f((lm - wm) * kLog2e);
+  const float wm = wave_max(ref);
+  // a lane whose reference is not the infinite one of the row adds nothing to it
+  float sum = wm == INFINITY ? (ref == INFINITY ? (float)ls : 0.f) : wm == -INFINITY ? 0.f : (float)ls * __builtin_amdgcn_exp2f((ref - wm) * kLog2e);
   sum = wave_sum(sum);
   const size_t at = (size_t)row * w.pieces + piece;
   if (lane == 0) w.ms[at] = make_float2(wm, sum);
@@ -280,7 +288,7 @@ constexpr int BF_PER = 8;                  // entries per thread and batch
 constexpr int BF_CAP = 1024;               // candidates held, those kept from batches before among them
 __global__ __launch_bounds__(BF_THREADS) void beam_final_kernel(BeamSelect a, BeamScratch w) {
   __shared__ double s_lse[kReorderBeams], s_score[kReorderBeams];
-  __shared__ int s_state[kReorderBeams];   // 1: the row's maximum is infinite, 2: the beam has ended
+  __shared__ int s_state[kReorderBeams];   // 1: the row has infinite logits, 2: the beam has ended
   __shared__ unsigned long long s_so[BF_CAP], s_key[BF_CAP], s_max[64], s_keep_so[kBeamKeep], s_keep_key[kBeamKeep];
   __shared__ int s_beam[BF_CAP], s_keep_beam[kBeamKeep], s_n;
   const int grp = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -310,17 +318,18 @@ __global__ __launch_bounds__(BF_THREADS) void beam_final_kernel(BeamSelect a, Be
     float2 v = lane < w.pieces ? ms[lane] : make_float2(-INFINITY, 0.f);
     const bool done = a.finished && a.finished[row] != 0;
     const float score = a.scores[row];
-    float m = v.x, s = 0.f;
+    float m = v.x;
+    double s = 0.0;
     for (int p = 64 + lane; p < w.pieces; p += 64) m = fmaxf(m, ms[p].x);
     m = wave_max(m);
     const float base = fabsf(m) < INFINITY ? m : 0.f;
     for (int p = lane;; v = ms[p]) {
-      if (v.x > -INFINITY) s += m == INFINITY ? (v.x == INFINITY ? v.y : 0.f) : v.y * expf(v.x - base);
+      if (v.x > -INFINITY) s += m == INFINITY ? (v.x == INFINITY ? (double)v.y : 0.0) : (double)v.y * (double)expf(v.x - base);
       if ((p += 64) >= w.pieces) break;
     }
-    s = wave_sum(s);
+    const float total = wave_sum((float)s);
     if (lane == 0) {
-      s_lse[b] = (double)base + log((double)s);
+      s_lse[b] = (double)base + log((double)total);
       s_state[b] = done ? 2 : m == INFINITY;
       s_score[b] = fabsf(score) < INFINITY ? (double)score : -(double)INFINITY;      // not finite: a beam that is not there
     }

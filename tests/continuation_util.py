@@ -109,6 +109,45 @@ def best(all_scores, n_groups, n_keep):
     return res
 
 
+def sum_error(vocab):
+    """Of cb_beam_select's sums of exponentials, relative: 31 float additions of a lane's round, 6 levels of a wavefront twice, exponentials and
+    joining factors of 2 units of 2^-24 each, 4 roundings; and for every unit of distance from the maximum up to 5 (3 for the exponent's subtraction,
+    product and constant, 2 for the factor where a reference moves, which is by 1 at least).  The distances, weighted by the probabilities, average to
+    at most ln vocab (sum p ln(max p / p) <= entropy), and a reference lags by at most 1 at two levels."""
+    return (31 + 12 + 6 + 4 + 5 * (2 + math.log(vocab))) * 2.0 ** -24
+
+
+def check_selection(got, logits, scores, n_groups, finished=None, end_token=0):
+    """got: the three results.  Scores within the sums' error and one rounding; beams and tokens as the definition gives them wherever no other
+    beam's score is nearer than twice the sums' error."""
+    got = [t.cpu() for t in got]
+    every, n_keep = beam_scores(logits, scores, finished, end_token), got[0].shape[1]
+    vocab, beams = logits.shape[1], logits.shape[0] // n_groups
+    wants = best(every, n_groups, min(n_keep + 1, beams * vocab))
+    top = every.topk(min(n_keep + 1, vocab), -1).values.cpu()         # of each beam: what a neighbour can be
+    every = every.cpu()
+    exact = 0
+    for g in range(n_groups):
+        want, seen = wants[g] + [(-math.inf, -1, -1)] * (n_keep + 1), set()
+        for i in range(n_keep):
+            s, b, t = float(got[0][g, i]), int(got[1][g, i]), int(got[2][g, i])
+            ws, wb, wt = want[i]
+            if ws == -math.inf:
+                assert (s, b, t) == (-math.inf, -1, -1), (g, i, s, b, t)
+                continue
+            tol = sum_error(vocab)
+            assert abs(s - ws) <= tol + abs(ws) * 2.0 ** -24, (g, i, s, ws)
+            assert (b, t) not in seen and 0 <= b < beams and 0 <= t < vocab
+            seen.add((b, t))
+            others = torch.cat((top[g * beams:g * beams + wb], top[g * beams + wb + 1:(g + 1) * beams])) - ws
+            if bool(((others.abs() <= 2 * tol) & (others != 0)).any()):
+                assert abs(float(every[g * beams + b, t]) - ws) <= 2 * tol
+            else:
+                exact += 1
+                assert (b, t) == (wb, wt), (g, i, (s, b, t), want[i])
+    return exact
+
+
 def attention_plan(m, n_groups, n_seqs, n_q, prefix, tail_stride):
     """The launches that cb_shared_prefix_attention chooses, asked of the library without a device; None: refused."""
     import ctypes
