@@ -459,6 +459,12 @@ def _empty(ctx: Context, stream, shape, dtype) -> torch.Tensor:
     return t
 
 
+def _room(ctx: Context, workspace: torch.Tensor) -> int:
+    """Bytes of a workspace, checked"""
+    assert workspace.get_device() == ctx.device.index and workspace.is_contiguous()
+    return workspace.numel() * workspace.element_size()
+
+
 def _cache_rows(ctx: Context, k: torch.Tensor, v: torch.Tensor) -> int:
     """Rows of a K and a V array [rows, Hkv, dh], checked"""
     shape = (k.shape[0], ctx.model.n_kv_heads, ctx.model.head_dim)
@@ -528,7 +534,7 @@ def cb_shared_prefix_attention(ctx: Context, q: torch.Tensor, n_groups: int, n_s
     status = _lib.cb_shared_prefix_attention(ctx._h, q.data_ptr(), n_groups, n_seqs, n_q, k_prefix.data_ptr(), v_prefix.data_ptr(),
                                              (C.c_int32 * n_groups)(*prefix_lens), prefix_stride, k_tail.data_ptr(), v_tail.data_ptr(),
                                              tail_stride, row_tail.data_ptr(), out.data_ptr(), workspace.data_ptr(),
-                                             workspace.numel(), _current_stream(ctx, stream))
+                                             _room(ctx, workspace), _current_stream(ctx, stream))
     _check(status, "cb_shared_prefix_attention")
     return out
 
@@ -559,7 +565,7 @@ def cb_beam_select(ctx: Context, logits: torch.Tensor, scores: torch.Tensor, n_g
         workspace = _empty(ctx, stream, max(256, cb_beam_select_workspace_bytes(ctx, n_groups, n_beams, vocab, n_keep)), torch.uint8)
     status = _lib.cb_beam_select(ctx._h, logits.data_ptr(), CB_BF16 if half else CB_F32, stride if rows > 1 else vocab, n_groups, n_beams,
                                  vocab, scores.data_ptr(), None if finished is None else finished.data_ptr(), end_token, n_keep,
-                                 out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                 out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), workspace.data_ptr(), _room(ctx, workspace),
                                  _current_stream(ctx, stream))
     _check(status, "cb_beam_select")
     return out
