@@ -452,10 +452,14 @@ def _fits(ctx: Context, t: torch.Tensor, dtype, shape) -> bool:
 
 
 def _empty(ctx: Context, stream, shape, dtype) -> torch.Tensor:
-    """A tensor of the current stream's that `stream` (None: the current one) uses: not handed out again before that stream is done"""
-    t = torch.empty(shape, dtype=dtype, device=ctx.device)
-    if stream is not None:
-        t.record_stream(stream)
+    """A tensor that `stream` (None: the current one) fills.  Its memory is that stream's own: memory that the current stream has freed may still be in
+    use by work that is waiting there.  Nor is it handed out again before the current stream, which may read the tensor, is done with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=ctx.device)
+    reader = torch.cuda.current_stream(ctx.device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=ctx.device)
+    t.record_stream(reader)
     return t
 
 
