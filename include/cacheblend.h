@@ -338,7 +338,7 @@ int cb_beam_select(cb_ctx *ctx, const void *logits, int32_t logits_dtype, int64_
  * of the beam's, on layers layer_begin .. layer_end - 1.  Rows behind stay as they were; a beam that is its own parent, or whose parent lies
  * outside 0 .. n_beams - 1 (beam_out's -1), keeps its slab.  Lengths are the parents' and in the old order: reordering them is the caller's.
  *   k_tail_layers, v_tail_layers : HOST arrays [n_layers] of device pointers to T [n_groups * n_beams * tail_stride, n_kv_heads,
- *               head_dim], all different
+ *               head_dim], none overlapping another; one that is given twice is CB_EINVAL
  *   parent    : int32 [n_groups * n_beams], counted within the group
  *   seq_len   : int32 [n_groups * n_beams] (0 .. tail_stride), or NULL: whole slabs
  * n_beams <= 64, n_groups <= 65535 (else CB_EUNSUPPORTED). */

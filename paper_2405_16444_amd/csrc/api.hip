@@ -7,6 +7,7 @@
 // host because the keep counts are inputs.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <cstdio>
@@ -1173,6 +1174,26 @@ int cb_beam_select(cb_ctx *c, const void *logits, int32_t logits_dtype, int64_t 
   return CB_OK;
 }
 
+namespace {
+// An array that is given twice would be read by some workgroups before and by others after it was moved.
+int check_all_differ(void *const *k, void *const *v, int n) {
+  auto at = [](const void *p) { return reinterpret_cast<uintptr_t>(p); };
+  // as a rule the layers lie one behind the other, all keys apart from all values
+  bool up = true;
+  for (int l = 1; up && l < n; ++l) up = at(k[l - 1]) < at(k[l]) && at(v[l - 1]) < at(v[l]);
+  if (up && (at(k[n - 1]) < at(v[0]) || at(v[n - 1]) < at(k[0]))) return CB_OK;
+  try {                                 // no exception may cross the C boundary
+    std::vector<uintptr_t> all;
+    all.reserve(2 * (size_t)n);
+    for (int l = 0; l < n; ++l) { all.push_back(at(k[l])); all.push_back(at(v[l])); }
+    std::sort(all.begin(), all.end());
+    return std::adjacent_find(all.begin(), all.end()) == all.end() ? CB_OK : CB_EINVAL;
+  } catch (...) {
+    return CB_ENOMEM;
+  }
+}
+}  // namespace
+
 int cb_beam_reorder(cb_ctx *c, void *const *k_tail_layers, void *const *v_tail_layers, int32_t layer_begin, int32_t layer_end,
                     int32_t n_groups, int32_t n_beams, int32_t tail_stride, const int32_t *parent, const int32_t *seq_len, void *stream) {
   if (!c || !k_tail_layers || !v_tail_layers || !parent) return CB_ENULL;
@@ -1188,6 +1209,7 @@ int cb_beam_reorder(cb_ctx *c, void *const *k_tail_layers, void *const *v_tail_l
   CB_TRY(check_stream(c, s));
   if (layer_begin == layer_end || tail_stride == 0 || n_beams == 1) return CB_OK;
   const int row_bytes = c->m.n_kv_heads * c->m.head_dim * (int)esize(c), nl = layer_end - layer_begin;
+  CB_TRY(check_all_differ(k_tail_layers + layer_begin, v_tail_layers + layer_begin, nl));
   ProfScope ps(c, s, CB_PROF_OTHER, 0, 4.0 * nl * (double)n_groups * n_beams * tail_stride * row_bytes);
   CB_HIP(launch_beam_reorder(k_tail_layers + layer_begin, v_tail_layers + layer_begin, nl, n_groups, n_beams, tail_stride, row_bytes,
                              parent, seq_len, s));

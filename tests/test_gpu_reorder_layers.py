@@ -1,0 +1,56 @@
+"""The layers' arrays that a reordering is given: each one once, in any order."""
+import ctypes as C
+import random
+
+import pytest
+import torch
+
+import continuation_util as U
+from gpu_util import announce
+
+pytestmark = pytest.mark.gpu
+
+EINVAL = -1
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2405_16444_amd as pkg
+    return pkg
+
+
+def test_an_array_that_is_given_twice_is_refused(P):
+    from paper_2405_16444_amd import binding
+    ctx = P.cb_create(U.model(2, 2, 64, "bf16", layers=4), 8)
+    t = U.normal((8, 12 * 5, 2, 64), 1, torch.bfloat16).cuda()
+    before = t.clone()
+    parent = torch.tensor([1, 2, 0] * 4, dtype=torch.int32, device="cuda")
+    at = [x.data_ptr() for x in t]
+
+    def call(k, v, begin=0, end=4):
+        return binding._lib.cb_beam_reorder(ctx._h, (C.c_void_p * 4)(*k), (C.c_void_p * 4)(*v), begin, end, 4, 3, 5, parent.data_ptr(), None, None)
+    for k, v in (([0, 1, 0, 3], [4, 5, 6, 7]), ([0, 1, 2, 3], [4, 5, 6, 6]), ([0, 1, 2, 3], [4, 5, 0, 7]), ([6, 1, 2, 3], [4, 5, 6, 7]),
+                 ([0, 1, 2, 4], [4, 5, 6, 7]), ([3, 2, 1, 0], [7, 6, 5, 3])):
+        announce("reorder, an array twice", k, v)
+        assert call([at[i] for i in k], [at[i] for i in v]) == EINVAL, (k, v)
+    torch.cuda.synchronize()
+    assert torch.equal(t, before)
+    # outside the range of layers it is not looked at
+    assert call([at[i] for i in (0, 1, 0, 0)], [at[i] for i in (4, 5, 4, 4)], 0, 2) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(t[2:4], before[2:4]) and not torch.equal(t[:2], before[:2])
+    P.cb_destroy(ctx)
+
+
+def test_layers_in_any_order(P):
+    ctx = P.cb_create(U.model(2, 2, 64, "bf16", layers=40), 8)
+    t = U.normal((80, 3, 7, 2, 64), 2, torch.bfloat16).cuda()
+    want = t[:, [2, 0, 0]]
+    order = list(range(80))
+    random.Random(3).shuffle(order)
+    for at in (list(range(80)), list(range(0, 80, 2)) + list(range(1, 80, 2)), order[:40] + order[40:]):
+        x = t.clone()
+        flat = [x[i].view(21, 2, 64) for i in at]
+        P.cb_beam_reorder(ctx, flat[:40], flat[40:], 1, torch.tensor([2, 0, 0], dtype=torch.int32, device="cuda"))
+        assert torch.equal(x, want)
+    P.cb_destroy(ctx)
