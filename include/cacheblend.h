@@ -341,6 +341,7 @@ int cb_beam_select(cb_ctx *ctx, const void *logits, int32_t logits_dtype, int64_
  *               head_dim], none overlapping another; one that is given twice is CB_EINVAL
  *   parent    : int32 [n_groups * n_beams], counted within the group
  *   seq_len   : int32 [n_groups * n_beams] (0 .. tail_stride), or NULL: whole slabs
+ * tail_stride = 0: nothing to do, the layers' pointers are ignored.
  * n_beams <= 64, n_groups <= 65535 (else CB_EUNSUPPORTED). */
 int cb_beam_reorder(cb_ctx *ctx, void *const *k_tail_layers, void *const *v_tail_layers, int32_t layer_begin, int32_t layer_end,
                     int32_t n_groups, int32_t n_beams, int32_t tail_stride, const int32_t *parent, const int32_t *seq_len, void *stream);

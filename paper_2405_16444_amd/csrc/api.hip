@@ -1199,7 +1199,7 @@ int cb_beam_reorder(cb_ctx *c, void *const *k_tail_layers, void *const *v_tail_l
   if (!c || !k_tail_layers || !v_tail_layers || !parent) return CB_ENULL;
   if (layer_begin < 0 || layer_end > c->m.n_layers || layer_begin > layer_end || n_groups < 1 || n_beams < 1 || tail_stride < 0)
     return CB_EINVAL;
-  for (int l = layer_begin; l < layer_end; ++l) {
+  for (int l = layer_begin; tail_stride > 0 && l < layer_end; ++l) {
     if (!k_tail_layers[l] || !v_tail_layers[l]) return CB_ENULL;
     if (!aligned(k_tail_layers[l], 16) || !aligned(v_tail_layers[l], 16) || k_tail_layers[l] == v_tail_layers[l]) return CB_EINVAL;
   }

@@ -54,3 +54,13 @@ def test_layers_in_any_order(P):
         P.cb_beam_reorder(ctx, flat[:40], flat[40:], 1, torch.tensor([2, 0, 0], dtype=torch.int32, device="cuda"))
         assert torch.equal(x, want)
     P.cb_destroy(ctx)
+
+
+def test_slabs_without_rows(P):
+    """as before the first new token, in caches that grow: nothing to do"""
+    ctx = P.cb_create(U.model(2, 2, 64, "bf16", layers=3), 8)
+    t = torch.zeros((3, 0, 2, 64), dtype=torch.bfloat16, device="cuda")
+    parent = torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    P.cb_beam_reorder(ctx, t, t.clone(), 1, parent)
+    P.cb_beam_reorder(ctx, list(t), list(t.clone()), 1, parent, parent)
+    P.cb_destroy(ctx)
