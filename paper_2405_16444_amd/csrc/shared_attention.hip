@@ -147,7 +147,8 @@ constexpr int shared_ring_bytes(int dh, int ks, int st) { return ks * st * 2 * S
 // RAGGED: several new tokens per continuation (n_q > 1), which see different tail rows and may be padding.  Else everything in the item's range
 // is seen by all of its queries.
 // NT: keys and values are loaded non-temporally.
-template <int DH, int QB, int KS, int ST, bool RAGGED, bool NT>
+// FOLD: the tails beside a wide launch, whose context pieces are joined here.
+template <int DH, int QB, int KS, int ST, bool RAGGED, bool NT, bool FOLD>
 __global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16_kernel(SharedAttn a) {
   constexpr int ROWB = DH * 2, CH = DH / 8, RPI = 1024 / ROWB, TB = SA_TILE * ROWB, LPT = SA_TILE / RPI, LPW = 2 * LPT / QB;
   constexpr int NKS = DH / 32, NCB = DH / 16, NQ = 16 * QB;
@@ -183,7 +184,7 @@ __global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16
   const int n_tiles = (kv_len + SA_TILE - 1) / SA_TILE;
   const int per = (int)(it.tail ? a.by_tail_pieces : a.by_ctx_pieces).div(n_tiles + pieces - 1);
   const int t_begin = piece * per, t_end = min(n_tiles, t_begin + per);
-  if (t_begin >= t_end && !a.fold) {
+  if (t_begin >= t_end && !FOLD) {
     store_empty(a, it, tid);
     return;
   }
@@ -377,7 +378,7 @@ __global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16
   float *dst = a.part_o + slot * DH + 4 * h;
   if constexpr (KS == 1) {
     if (m >= it.m_end) return;
-    if (a.fold) return fold_and_store<NCB, DH>(a, it.row0 + r, kvh, m - r * g, 4 * h, top, row_sum, oacc);
+    if constexpr (FOLD) return fold_and_store<NCB, DH>(a, it.row0 + r, kvh, m - r * g, 4 * h, top, row_sum, oacc);
     if (h == 0) *reinterpret_cast<float2 *>(a.part_ml + slot * 2) = make_float2(top, row_sum);
 #pragma unroll
     for (int c = 0; c < NCB; ++c) *reinterpret_cast<f32x4 *>(dst + 16 * c) = oacc[c];
@@ -413,7 +414,7 @@ __global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16
         acc[c] = s == 0 ? w * v : acc[c] + w * v;
       }
     }
-    if (a.fold) return fold_and_store<CPW, DH>(a, it.row0 + r, kvh, m - r * g, 16 * ks * CPW + 4 * h, top, l, acc);
+    if constexpr (FOLD) return fold_and_store<CPW, DH>(a, it.row0 + r, kvh, m - r * g, 16 * ks * CPW + 4 * h, top, l, acc);
     if (h == 0 && ks == 0) *reinterpret_cast<float2 *>(a.part_ml + slot * 2) = make_float2(top, l);
 #pragma unroll
     for (int c = 0; c < CPW; ++c) *reinterpret_cast<f32x4 *>(dst + 16 * (ks * CPW + c)) = acc[c];
@@ -657,25 +658,29 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedAttn a) {
   store4<T>((T *)a.o + ((size_t)r * a.hq + hd) * DH + c * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
-template <int DH, int QB, int KS, int ST, bool RAGGED, bool NT = false>
-hipError_t launch_bf16(const SharedAttn &a, unsigned grid, hipStream_t s) {
+template <int DH, int QB, int KS, int ST, bool RAGGED, bool NT, bool FOLD>
+hipError_t launch_one(const SharedAttn &a, unsigned grid, hipStream_t s) {
   constexpr int smem = shared_ring_bytes(DH, KS, ST) + QB * KS * 16 * 8;
   static_assert(shared_ring_bytes(DH, KS, ST) >= QB * KS * (DH / 16) * 1024 || KS == 1, "the join fits in the rings' place");
   static std::once_flag once;
   std::call_once(once, [] {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&shared_attn_bf16_kernel<DH, QB, KS, ST, RAGGED, NT>),
+    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&shared_attn_bf16_kernel<DH, QB, KS, ST, RAGGED, NT, FOLD>),
                               hipFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
-  hipLaunchKernelGGL((shared_attn_bf16_kernel<DH, QB, KS, ST, RAGGED, NT>), dim3(grid), dim3(64 * QB * KS), smem, s, a);
+  hipLaunchKernelGGL((shared_attn_bf16_kernel<DH, QB, KS, ST, RAGGED, NT, FOLD>), dim3(grid), dim3(64 * QB * KS), smem, s, a);
   return hipGetLastError();
+}
+template <int DH, int QB, int KS, int ST, bool RAGGED>
+hipError_t launch_bf16(const SharedAttn &a, unsigned grid, hipStream_t s) {
+  return a.fold ? launch_one<DH, QB, KS, ST, RAGGED, false, true>(a, grid, s) : launch_one<DH, QB, KS, ST, RAGGED, false, false>(a, grid, s);
 }
 template <int DH>
 hipError_t launch_bf16_qb(const SharedAttn &a, unsigned grid, hipStream_t s) {
   // as many tiles at a time as the wavefronts leave; one new token: two workgroups to a CU, which hide each other's loads
-  if (a.n_q == 1 && a.stream) switch (a.qb) {
-      case 1: return launch_bf16<DH, 1, 4, 1, false, true>(a, grid, s);
-      case 2: return launch_bf16<DH, 2, 4, 1, false, true>(a, grid, s);
-      case 4: return launch_bf16<DH, 4, 2, 2, false, true>(a, grid, s);
+  if (a.stream) switch (a.qb) {
+      case 1: return launch_one<DH, 1, 4, 1, false, true, false>(a, grid, s);
+      case 2: return launch_one<DH, 2, 4, 1, false, true, false>(a, grid, s);
+      case 4: return launch_one<DH, 4, 2, 2, false, true, false>(a, grid, s);
     }
   if (a.n_q == 1) switch (a.qb) {
       case 1: return launch_bf16<DH, 1, 4, 1, false>(a, grid, s);
@@ -784,16 +789,20 @@ size_t shared_attention_floats(SharedAttn a, int max_ctx) {
   return std::max(narrow, floats_of(a));
 }
 
+// One query block reads everything once: contexts that the caches will hardly hold until the next step are not kept in them.  Eight beams
+// over 65536 keys (268 MB) 61 -> 56 us, 32896 keys 33.0 -> 31.7, four beams 30.6 -> 27.2, 28000 keys 25.0 -> 23.6; 20000 keys (82 MB) 21.9 ->
+// 22.3, 12000 keys 15.2 -> 17.1.
+static bool past_the_caches(const SharedAttn &a) {
+  double keys = 0;
+  for (int grp = 0; grp < a.n_groups; ++grp) keys += a.ctx_len[grp];
+  return !a.wide && a.n_q == 1 && a.qb <= 4 && a.ctx_blocks == 1 && keys * a.hkv * a.dh * 4 >= 96.0 * (1 << 20);
+}
+
 hipError_t launch_shared_attention(SharedAttn a, float *scratch, hipStream_t s) {
   a.part_o = scratch;
   a.part_ml = scratch + (a.tail_slot0 + (size_t)a.rows * a.hq * a.tail_pieces) * a.dh;
   a.scale_log2e = kLog2e / sqrtf((float)a.dh);
-  // One query block reads everything once: contexts that the caches will hardly hold until the next step are not kept in them.  Eight beams
-  // over 65536 keys (268 MB) 61 -> 56 us, 32896 keys 33.0 -> 31.7, four beams 30.6 -> 27.2, 28000 keys 25.0 -> 23.6; 20000 keys (82 MB) 21.9 ->
-  // 22.3, 12000 keys 15.2 -> 17.1.
-  double keys = 0;
-  for (int grp = 0; grp < a.n_groups; ++grp) keys += a.ctx_len[grp];
-  a.stream = !a.wide && a.ctx_blocks == 1 && keys * a.hkv * a.dh * 4 >= 96.0 * (1 << 20);
+  a.stream = past_the_caches(a);
   if (a.wide) {
     const int rows = a.n_seqs * a.n_q;
     const size_t q_row = (size_t)a.hq * a.dh * 2, slab = (size_t)a.ctx_stride * a.hkv * a.dh * 2, slots = (size_t)a.hkv * a.ctx_rows * a.ctx_pieces;
@@ -831,7 +840,8 @@ extern "C" int cb_internal_shared_plan(int dtype, int hq, int hkv, int dh, int n
   a.dtype = dtype; a.hq = hq; a.hkv = hkv; a.dh = dh;
   a.n_groups = n_groups; a.n_seqs = n_seqs; a.n_q = n_q; a.tail_stride = tail_stride;
   if (!cb::shared_attention_plan(a, max_ctx)) return 0;
-  const int v[] = {a.wide, a.fold, a.qb, a.ctx_blocks, a.ctx_pieces, a.tail_blocks, a.tail_pieces};
-  std::copy(v, v + 7, out);
+  for (int grp = 0; grp < std::min(n_groups, cb::kSharedGroups); ++grp) a.ctx_len[grp] = max_ctx;
+  const int v[] = {a.wide, a.fold, a.qb, a.ctx_blocks, a.ctx_pieces, a.tail_blocks, a.tail_pieces, dtype != 0 && cb::past_the_caches(a)};
+  std::copy(v, v + 8, out);
   return 1;
 }

@@ -152,7 +152,7 @@ def attention_plan(m, n_groups, n_seqs, n_q, prefix, tail_stride):
     """The launches that cb_shared_prefix_attention chooses, asked of the library without a device; None: refused."""
     import ctypes
     from paper_2405_16444_amd.binding import _lib
-    out = (ctypes.c_int * 7)()
+    out = (ctypes.c_int * 8)()
     if not _lib.cb_internal_shared_plan(int(m.dtype == "bf16"), m.n_q_heads, m.n_kv_heads, m.head_dim, n_groups, n_seqs, n_q, prefix, tail_stride, out):
         return None
-    return SimpleNamespace(**dict(zip(("wide", "fold", "qb", "ctx_blocks", "ctx_pieces", "tail_blocks", "tail_pieces"), out)))
+    return SimpleNamespace(**dict(zip(("wide", "fold", "qb", "ctx_blocks", "ctx_pieces", "tail_blocks", "tail_pieces", "stream"), out)))

@@ -1,4 +1,7 @@
 """The launches of attention over a shared context, asked of the library's planner without a device."""
+import itertools
+import re
+
 import pytest
 
 import continuation_util as U
@@ -37,3 +40,17 @@ def test_the_largest_launch_is_refused():
     assert U.attention_plan(m, 64, 4096, 1, 0, 1) is None and U.attention_plan(m, 64, 4096, 1, 40, 1) is None
     assert U.attention_plan(m, 64, 4096, 1, 40, 0) is not None and U.attention_plan(m, 64, 3900, 1, 40, 1) is not None
     assert U.attention_plan(m, 64, 4097, 1, 40, 0) is None
+
+
+def test_every_kernel_that_is_built_is_reached_by_some_plan():
+    from paper_2405_16444_amd import build
+    names = re.findall(rb"shared_attn_bf16_kernelILi(\d+)ELi(\d)ELi\dELi\dELb(\d)ELb(\d)ELb(\d)E", open(build.LIB_PATH, "rb").read())
+    built = {tuple(map(int, n)) for n in names}                      # head_dim, query blocks, several tokens, past the caches, folding
+    reached = set()
+    for dh, (hq, hkv), n_seqs, n_q, prefix in itertools.product(
+            (64, 128), ((32, 32), (32, 8), (64, 8), (32, 1), (64, 1), (128, 1), (5, 5), (48, 8)), (1, 3, 8, 64, 128, 256, 512, 1024),
+            (1, 2, 4, 8, 64), (40, 600, 3000, 30000, 100000)):
+        p = U.attention_plan(U.model(hq, hkv, dh, "bf16"), 1, n_seqs, n_q, prefix, 32)
+        if p is not None:
+            reached.add((dh, p.qb, int(n_q > 1), p.stream, p.fold))
+    assert len(built) == 38 and built == reached, (sorted(built - reached), sorted(reached - built))
