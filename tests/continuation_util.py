@@ -156,3 +156,40 @@ def attention_plan(m, n_groups, n_seqs, n_q, prefix, tail_stride):
     if not _lib.cb_internal_shared_plan(int(m.dtype == "bf16"), m.n_q_heads, m.n_kv_heads, m.head_dim, n_groups, n_seqs, n_q, prefix, tail_stride, out):
         return None
     return SimpleNamespace(**dict(zip(("wide", "fold", "qb", "ctx_blocks", "ctx_pieces", "tail_blocks", "tail_pieces", "stream"), out)))
+
+
+# Shapes of attention that together reach every bf16 kernel: query heads, key/value heads, context rows, continuations, new tokens of each, and what the
+# plan makes of them (query blocks, past the caches, folding).  Contexts past the caches have 96 MB and a little.
+def plan_shapes(dh):
+    far = (96 << 20) // (16 * dh * 4) + 457
+    return [((16, 16, far, 3, 1), (1, 1, 0)), ((64, 16, far, 7, 1), (2, 1, 0)), ((64, 16, far, 12, 1), (4, 1, 0)),
+            ((8, 2, 731, 3, 1), (1, 0, 0)), ((8, 2, 1999, 7, 1), (2, 0, 0)), ((8, 2, 2501, 12, 1), (4, 0, 0)), ((8, 2, 2999, 30, 1), (8, 0, 0)),
+            ((64, 8, 611, 512, 1), (1, 0, 1)), ((32, 1, 437, 1024, 1), (2, 0, 1)), ((64, 1, 437, 512, 1), (4, 0, 1)), ((128, 1, 437, 256, 1), (8, 0, 1)),
+            ((5, 5, 731, 2, 5), (1, 0, 0)), ((6, 3, 1999, 2, 7), (2, 0, 0)), ((4, 4, 1501, 3, 20), (4, 0, 0)), ((4, 2, 999, 3, 20), (8, 0, 0)),
+            ((64, 8, 611, 256, 2), (1, 0, 1)), ((64, 8, 611, 128, 4), (2, 0, 1)), ((64, 8, 611, 64, 8), (4, 0, 1)), ((64, 8, 1003, 16, 64), (8, 0, 1))]
+
+
+def coded_values(rows, heads, dh, first=0):
+    """Values [rows, heads, dh] in which every tile of 32 rows has a channel of its own (the next tiles after dh of them take the same again): an output
+    channel is the sum of a few tiles' probabilities, and a tile that is lost or taken twice changes it by its share of them."""
+    row = torch.arange(rows)
+    v = torch.zeros((rows, heads, dh))
+    v[row, :, (first + row // 32) % dh] = (1 + (row * 37 % 61) / 128)[:, None]
+    return v
+
+
+def border_rows(prefix):
+    return [0, 31, 32, 33, 63, 64, prefix // 2, prefix - 2, prefix - 1]
+
+
+def towards_borders(q, kp, kt, prefix):
+    """(q, kp, kt) in which the context's border rows and all tail rows have most of the probability: queries share a direction per key/value head, and
+    these keys lie along it, for scores of 1.25 ln prefix beside the others' of less than 1.  Rows behind the context would take everything."""
+    hkv, dh = kp.shape[2:]
+    way = normal((hkv, dh), 97).sign().to(q.device)
+    q = (way.repeat_interleave(q.shape[1] // hkv, 0) + 0.3 * q.float()).to(q.dtype)
+    along = 1.25 * math.log(prefix) / dh ** 0.5 * way
+    kp, kt = (0.3 * kp.float()).to(kp.dtype), (0.3 * kt.float() + along).to(kt.dtype)
+    kp[0, border_rows(prefix)] = (kp[0, border_rows(prefix)].float() + along).to(kp.dtype)
+    kp[0, prefix:] = (8 * way).to(kp.dtype)
+    return q, kp, kt

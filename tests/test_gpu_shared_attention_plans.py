@@ -88,3 +88,40 @@ def test_more_workgroups_than_a_launch_numbers_are_refused(P):
     p, lens = buf.data_ptr(), (C.c_int32 * 64)(*[40] * 64)
     assert binding._lib.cb_shared_prefix_attention(ctx._h, p, 64, 4096, 1, p, p, lens, 40, p, p, 1, p, p, p, 1 << 60, None) == -4
     P.cb_destroy(ctx)
+
+
+EVERY = [(dh, *shape) for dh in (64, 128) for shape, _ in U.plan_shapes(dh)]
+
+
+@pytest.mark.parametrize("dh,hq,hkv,prefix,n_seqs,n_q", EVERY)
+def test_every_tile_counts_once(P, dh, hq, hkv, prefix, n_seqs, n_q):
+    """values that give every tile of the context, and of the tails, a channel which few others share"""
+    m, stride = U.model(hq, hkv, dh, "bf16"), n_q + 20
+    rt = ragged(n_seqs, n_q, stride, prefix)
+    announce("every tile counts", dh, hq, hkv, prefix, n_seqs, n_q)
+    q, kp, _, kt, _, r = inputs(m, [prefix], n_seqs, n_q, stride, rt, 81, prefix)
+    vp = U.coded_values(prefix, hkv, dh).to(torch.bfloat16)[None].cuda()
+    vt = U.coded_values(stride, hkv, dh, prefix // 32 + 1).to(torch.bfloat16)[None].expand(n_seqs, -1, -1, -1).contiguous().cuda()
+    check(P, m, q, kp, vp, prefix, kt, vt, r, n_seqs, n_q)
+
+
+@pytest.mark.parametrize("dh,hq,hkv,prefix,n_seqs,n_q", EVERY)
+def test_rows_at_the_borders_count(P, dh, hq, hkv, prefix, n_seqs, n_q):
+    """a few context rows, at tile borders and the ends, and all tail rows have most of the probability"""
+    m, stride = U.model(hq, hkv, dh, "bf16"), n_q + 20
+    rt = ragged(n_seqs, n_q, stride, prefix + 1)
+    announce("border rows", dh, hq, hkv, prefix, n_seqs, n_q)
+    q, kp, vp, kt, vt, r = inputs(m, [prefix], n_seqs, n_q, stride, rt, 91, prefix + 40)
+    q, kp, kt = U.towards_borders(q, kp, kt, prefix)
+    check(P, m, q, kp, vp, prefix, kt, vt, r, n_seqs, n_q)
+
+
+def check(P, m, q, kp, vp, prefix, kt, vt, r, n_seqs, n_q):
+    ctx = P.cb_create(m, 8)
+    out = call(P, ctx, q, kp, vp, [prefix], kt, vt, r, n_seqs, n_q)
+    ref, bound = U.attention(q, kp, vp, [prefix], kt, vt, r.cpu(), n_seqs, n_q, m.dtype)
+    off = (out.double() - ref).abs()
+    assert bool(torch.isfinite(out).all()) and bool((off <= bound).all()), float((off / bound.clamp_min(1e-30)).max())
+    assert not bool(out[r < 0].any())
+    assert same(call(P, ctx, q, kp, vp, [prefix], kt, vt, r, n_seqs, n_q, out=q), out)      # over the queries
+    P.cb_destroy(ctx)
