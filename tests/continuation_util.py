@@ -119,7 +119,8 @@ def sum_error(vocab):
 
 def check_selection(got, logits, scores, n_groups, finished=None, end_token=0):
     """got: the three results.  Scores within the sums' error and one rounding; beams and tokens as the definition gives them wherever no other
-    beam's score is nearer than twice the sums' error."""
+    beam's score is nearer than twice the sums' error.  Beams of the same logits and score have the same sums; of the same logits in another order they
+    do not, as float additions depend on it."""
     got = [t.cpu() for t in got]
     every, n_keep = beam_scores(logits, scores, finished, end_token), got[0].shape[1]
     vocab, beams = logits.shape[1], logits.shape[0] // n_groups
@@ -127,6 +128,10 @@ def check_selection(got, logits, scores, n_groups, finished=None, end_token=0):
     top = every.topk(min(n_keep + 1, vocab), -1).values.cpu()         # of each beam: what a neighbour can be
     every = every.cpu()
     exact = 0
+    ended = torch.zeros_like(scores) if finished is None else finished.to(scores)
+    ids = {}
+    kind = torch.tensor([ids.setdefault(row.tobytes(), len(ids)) for row in
+                         torch.cat((logits.float() + 0.0, scores[:, None], ended[:, None]), 1).cpu().numpy()])
     for g in range(n_groups):
         want, seen = wants[g] + [(-math.inf, -1, -1)] * (n_keep + 1), set()
         for i in range(n_keep):
@@ -139,8 +144,9 @@ def check_selection(got, logits, scores, n_groups, finished=None, end_token=0):
             assert abs(s - ws) <= tol + abs(ws) * 2.0 ** -24, (g, i, s, ws)
             assert (b, t) not in seen and 0 <= b < beams and 0 <= t < vocab
             seen.add((b, t))
-            others = torch.cat((top[g * beams:g * beams + wb], top[g * beams + wb + 1:(g + 1) * beams])) - ws
-            if bool(((others.abs() <= 2 * tol) & (others != 0)).any()):
+            mine = slice(g * beams, (g + 1) * beams)
+            near = ((top[mine] - ws).abs() <= 2 * tol) & (kind[mine] != kind[g * beams + wb])[:, None]
+            if bool(near.any()):
                 assert abs(float(every[g * beams + b, t]) - ws) <= 2 * tol
             else:
                 exact += 1
