@@ -14,7 +14,8 @@ namespace {
 // row, so that the position, and with it the (cos, sin) values a lane needs, are the same for all of the heads it walks
 // through.  A lane holds the 16-byte vectors at channel p N and dh/2 + p N of a head: both rotary orders then find their
 // pairs within the lane, the adjacent one inside each vector, the half-split one across the two.
-// 4099 rows of 64 + 2 x 8 heads of 128 with norms 33.7 us = 5.0 TB/s, the rate of a copy; 8 rows 3.3 us, an empty launch being 2.6.
+// 4099 rows of 64 + 2 x 8 heads of 128 with norms 33.7 us = 5.0 TB/s, the rate of a copy; 8 rows 3.2 us, an empty launch being 2.6; 4099 rows of 4 + 2 x 2
+// float heads of 64 5.6 us.
 // ---------------------------------------------------------------------------
 template <typename T, int DH, bool HALF>
 __global__ __launch_bounds__(256) void qkv_norm_rope_kernel(QkvRows a) {
@@ -466,7 +467,8 @@ BeamScratch beam_scratch(int rows, int vocab, int n_keep, void *base, size_t *by
 // ---------------------------------------------------------------------------
 // Reordering in place.  Every 16-byte piece of a row is moved between the beams of its group by one lane, which reads what all of them will
 // receive before it writes any of it: no second buffer, no order between workgroups.  A beam that stays where it is moves nothing.
-// 640 slabs of 80 rows of 2 KB 261 us = 5.0 TB/s, the rate of a copy.
+// 640 slabs of 80 rows of 2 KB 261 us = 5.0 TB/s, the rate of a copy; 32 slabs a layer as 16 beams 299, as 32 beams 356 (a lane holds a piece of
+// every beam, so fewer wavefronts fit).
 // ---------------------------------------------------------------------------
 constexpr int kReorderLayers = 128;
 struct ReorderArgs {
@@ -549,7 +551,9 @@ hipError_t launch_beam_reorder(void *const *k_layers, void *const *v_layers, int
     for (int i = 0; i < 2 * kReorderLayers; ++i) a.layer[i] = (i & 1 ? v_layers : k_layers)[l0 + std::min(i / 2, nl - 1)];
     // Whole slabs would need `need` workgroups each, tails fill them in part: small arrays take as many workgroups as the chip holds at a time (64
     // slabs of 24 of 128 rows 8.4 us, with 4096 workgroups 10.4), large ones enough to keep it busy to the end (640 of 80 of 96 rows
-    // 261 us with 16384, 279 with 4096).
+    // 261 us with 16384, 279 with 4096).  2048 against 16384, by whole slabs' workgroups: 4096 8.4 / 10.6 us, 7680 (24 of 128 rows) 9.6 / 17 and
+    // 15.8 / 30, 8192 (64 of 128) 41 / 44; 15360 (40 of 96) 73 / 81, 16384 (64 of 128) 93 / 81, (8 of 512) 8 / 20, (400 of 512) 68 / 62, 30720 (40 of
+    // 96) 133 / 122: beyond 8192 it depends on how full the tails are.
     const long need = ((long)tail_stride * chunks + 255) / 256, others = (long)n_groups * nl * 2;
     const long most = need * others <= 8192 ? 2048 : 16384;
     const dim3 grid((unsigned)std::max<long>(1, std::min<long>(need, most / others)), n_groups, 2 * nl);

@@ -140,8 +140,9 @@ __device__ __forceinline__ void store_empty(const SharedAttn &a, const Item &it,
 // block, whatever QB.  (With two blocks unrolled in one wavefront eight beams over 3136 keys took 10.0 us instead of 8.7: each
 // instruction of a short piece is executed once, so the time is that of fetching them.)  The QB wavefronts of a tile share its loads;
 // the KS tiles' results are joined in LDS.
-// Eight beams, 32 query heads over 8: 3136 keys 9.0 us, of which the burst of all loads is 2; 32896 keys 31.7 us = 4.4 TB/s, 65536
-// keys 56 us = 4.8 TB/s.
+// Eight beams, 32 query heads over 8: 3136 keys 8.8 us (their bytes at the copy rate: 2.6); 32896 keys 31 us = 4.4 TB/s, 65536
+// keys 56 us = 4.8 TB/s.  Several tokens each: 8 x 5 over 3136 keys 18.5 us, 4 x 5 of 64 heads over 8000 28.2, 4 requests of 4 x 16 of 56 heads over
+// 2300 84.
 // ---------------------------------------------------------------------------
 constexpr int shared_ring_bytes(int dh, int ks, int st) { return ks * st * 2 * SA_TILE * dh * 2; }
 // RAGGED: several new tokens per continuation (n_q > 1), which see different tail rows and may be padding.  Else everything in the item's range
@@ -300,7 +301,8 @@ __global__ __launch_bounds__(64 * QB * KS, RAGGED ? 2 : 4) void shared_attn_bf16
     for (int e = 0; e < 8; ++e) {
       const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 2][e & 3], scale, neg_mc));
       psum += p;
-      pf[e] = (bf16)p;                                    // the matrix cores' operand type; the sum keeps the float
+      pf[e] = (bf16)p;                                    // the matrix cores' operand type, as in the fusing pass; the sum keeps the float.  It
+                                                          // adds a second error as large as the output's own rounding: 0.0017 -> 0.0024 (2-norm)
     }
     row_sum += psum;
 #pragma unroll
@@ -451,7 +453,7 @@ __device__ __forceinline__ void join_and_store(const SharedAttn &a, const Item &
 // ---------------------------------------------------------------------------
 // float, v_mfma_f32_16x16x4_f32: the same items with 16 queries per workgroup and K, V straight from memory (a float model's
 // caches fit L2).  The contraction index a lane supplies in MFMA s is 4 (lane / 16) + s for both products.  Four beams over 544 keys
-// of the 4 x 64 model 5.6 us.
+// of the 4 x 64 model 5.8 us, over 8000 6.1; 8 x 64 tokens over 2000 keys 38, with 8 heads of 128 74.
 // ---------------------------------------------------------------------------
 constexpr int SF_NW = 4;
 template <int DH>
@@ -789,9 +791,12 @@ size_t shared_attention_floats(SharedAttn a, int max_ctx) {
   return std::max(narrow, floats_of(a));
 }
 
-// One query block reads everything once: contexts that the caches will hardly hold until the next step are not kept in them.  Eight beams
-// over 65536 keys (268 MB) 61 -> 56 us, 32896 keys 33.0 -> 31.7, four beams 30.6 -> 27.2, 28000 keys 25.0 -> 23.6; 20000 keys (82 MB) 21.9 ->
-// 22.3, 12000 keys 15.2 -> 17.1.
+// One query block reads everything once, so contexts too large to be found in the caches by a later call need not be put there.  Where that begins
+// depends on what is called in between.  Three contexts in turn, eight beams: 65536 keys (268 MB) 61 -> 56 us, 32896 keys 33.0 -> 31.7, 28000 keys
+// 25.0 -> 23.6; 20000 keys (82 MB) 21.9 -> 22.3, 12000 keys 15.2 -> 17.1, which the bound of 96 MB follows.  One context again and again never
+// gains (3136 keys 8.6 -> 8.7, 32896 keys 25.3 -> 29.8); contexts that always come from memory, as when a step reads one for each of many layers, gain at
+// every length: 3136 keys 10.3 -> 10.0, 8000 14.6 -> 13.6, 16000 19.5 -> 17.6, 32896 32.7 -> 30.4.  The call does not know what is called in between;
+// the bound is that of the first of these cases.
 static bool past_the_caches(const SharedAttn &a) {
   double keys = 0;
   for (int grp = 0; grp < a.n_groups; ++grp) keys += a.ctx_len[grp];
