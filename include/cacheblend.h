@@ -304,10 +304,9 @@ int cb_qkv_norm_rope(cb_ctx *ctx, const void *q, int64_t q_stride, const void *k
  * A padding row, and one that sees no key at all, gets zeros.  Hidden rows have no influence, whatever they hold (infinities and
  * NaN included).  Softmax statistics and sums are float; results do not depend on which continuations share the call but for
  * the order of additions.  prefix_stride = 0 / tail_stride = 0: no contexts / tails, their pointers are ignored.
- * A launch takes 64 groups.  In it the rows x n_q_heads are at most 2^23, and so many key/value heads of contexts and tails (one for each 16 to 128
- * of their queries) that its threads, 256 or 512 each, can be numbered with 32 bits: rows x n_q_heads <= 2^22 is always covered (else
- * CB_EUNSUPPORTED).  The workspace bytes for max_prefix hold for every shorter context;
- * 0: arguments out of range. */
+ * min(n_groups, 64) * n_seqs * n_q * n_q_heads <= 2^22 is always covered; up to 2^23 unless the workgroups of a launch (one for a key/value head
+ * of each context and tail, more for more than 16 .. 128 queries of it), of 256 or 512 threads, would have 2^32 threads (else
+ * CB_EUNSUPPORTED).  The workspace bytes for max_prefix hold for every shorter context; 0: arguments out of range. */
 size_t cb_shared_prefix_workspace_bytes(const cb_ctx *ctx, int32_t n_groups, int32_t n_seqs, int32_t n_q, int32_t max_prefix,
                                         int32_t tail_stride);
 int cb_shared_prefix_attention(cb_ctx *ctx, const void *q, int32_t n_groups, int32_t n_seqs, int32_t n_q, const void *k_prefix,

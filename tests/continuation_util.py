@@ -127,7 +127,6 @@ def check_selection(got, logits, scores, n_groups, finished=None, end_token=0):
     wants = best(every, n_groups, min(n_keep + 1, beams * vocab))
     top = every.topk(min(n_keep + 1, vocab), -1).values.cpu()         # of each beam: what a neighbour can be
     every = every.cpu()
-    exact = 0
     ended = torch.zeros_like(scores) if finished is None else finished.to(scores)
     ids = {}
     kind = torch.tensor([ids.setdefault(row.tobytes(), len(ids)) for row in
@@ -149,9 +148,7 @@ def check_selection(got, logits, scores, n_groups, finished=None, end_token=0):
             if bool(near.any()):
                 assert abs(float(every[g * beams + b, t]) - ws) <= 2 * tol
             else:
-                exact += 1
                 assert (b, t) == (wb, wt), (g, i, (s, b, t), want[i])
-    return exact
 
 
 def attention_plan(m, n_groups, n_seqs, n_q, prefix, tail_stride):
